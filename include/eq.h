@@ -273,6 +273,132 @@ int eq_gemm_codes(const eq_layer *L, const uint8_t *codes, const uint16_t *x, ui
 int eq_decode_gemm(const eq_layer *L, const uint16_t *x, uint32_t B, const uint16_t *bias,
                    float *y, void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * The attention side of a block: between the query/key/value projections and
+ * the output projection.  Keys and values are held in 4 bits in a paged cache.
+ *
+ * Number format: E2M1 codes (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6), and a scale byte b for each group that stands for
+ * 2^(b - 127).  A key has one group for every 32 channels, a value one group
+ * for all of a head's channels.  With A the largest magnitude of a group and
+ * 2^a <= A < 2^(a+1): b - 127 = a - 2, or a - 1 where A >= 1.75 2^a, clamped to
+ * [-103, 125] (b in [24, 252]); the codes are the group's values over 2^(b -
+ * 127), rounded to nearest with ties to even, in magnitude at most 6.  A group
+ * that holds an infinity or NaN has b = 255 and reads as NaN.  A cached token
+ * takes D + D/32 + 1 bytes for each head of D channels (4.16 bits a value at
+ * D = 128).
+ *
+ * Page: page_tokens tokens of all kv_heads heads, head by head, each head's
+ * part padded to a multiple of 128 bytes.  With n = page_tokens, a head's part
+ * holds, for token t of the page,
+ *   key codes     n x D/2 bytes: channel c in byte t D/2 + c/2, even c in the
+ *                 low four bits
+ *   value codes   n/32 x D x 16 bytes: channel c in byte (t/32 D + c) 16 +
+ *                 t%32/2, even t in the low four bits
+ *   key scales    n x D/32 bytes: channels 32 g .. of token t in byte
+ *                 t/16 (D/2) + (t%4 D/32 + g) 4 + t%16/4
+ *   value scales  n bytes
+ * Value codes lie along the tokens because that is the axis over which
+ * attention sums them; the key scales lie as the matrix instructions take
+ * them.  What a page holds behind a sequence's last token does not matter.
+ */
+#define EQ_F32 0
+#define EQ_BF16 1
+
+typedef struct eq_kv_cache {
+  uint8_t *pages;       /* device: n_pages x eq_kv_page_bytes(), 128-byte aligned  */
+  uint32_t n_pages;     /* >= 1                                                    */
+  uint32_t page_tokens; /* a power of two, 32 to 4096                              */
+  uint32_t kv_heads;    /* 1 to 1024                                               */
+  uint32_t head_dim;    /* D: 64 or 128                                            */
+} eq_kv_cache;
+
+/* The tokens of a call.  Sequence s has the rows seq_start[s] .. seq_start[s +
+ * 1] - 1 of the call's dense inputs and outputs; they are the last ones of its
+ * kv_len[s] tokens (new ones included), so row seq_start[s] + i is at position
+ * kv_len[s] - (seq_start[s + 1] - seq_start[s]) + i.  Position p is in page
+ * page_table[s max_pages + p / page_tokens].  The arrays are read on the
+ * device, so a captured graph may replay with other lengths and pages; what
+ * the launch depends on is in the host fields, which bound them.  Rows,
+ * positions and pages outside the bounds (a page number below 0 marks a page
+ * that is not there) are skipped: append and read leave out such tokens,
+ * attention takes them for absent. */
+typedef struct eq_kv_batch {
+  const int32_t *seq_start;  /* device: n_seqs + 1, ascending from >= 0            */
+  const int32_t *kv_len;     /* device: n_seqs                                     */
+  const int32_t *page_table; /* device: n_seqs x max_pages                         */
+  uint32_t n_seqs;           /* at most 65535                                      */
+  uint32_t max_pages;
+  uint32_t n_tokens;         /* rows of the dense arrays                           */
+  uint32_t max_new;          /* bound of a sequence's rows                         */
+  uint32_t max_len;          /* bound of kv_len (at most max_pages page_tokens)    */
+} eq_kv_batch;
+
+/* Rotation of the first `dims` channels (a multiple of 16, at most D) of a
+ * head at position p by cos and sin [rows][dims / 2] (device, fp32, 16-byte
+ * aligned): channel pairs (c, c + dims/2), or (2c, 2c + 1) when `pairs` is
+ * set, go to (x cos - y sin, y cos + x sin).  A position outside the table
+ * takes the nearest row's. */
+typedef struct eq_rope {
+  const float *cos, *sin;
+  uint32_t rows, dims, pairs;
+} eq_rope;
+
+/* Norm of every query and key head and its rotation: y = rot(x / sqrt(mean
+ * x^2 + eps) w), in fp32, rounded once to BF16.  q: `tokens` rows of q_heads x
+ * head_dim elements of `dtype` (EQ_F32 or EQ_BF16), q_stride elements apart;
+ * q_out: contiguous [tokens][q_heads][head_dim]; k likewise (k_heads may be
+ * 0).  q_weight, k_weight: BF16 [head_dim] (2-byte aligned) or NULL for no
+ * norm.  rope: NULL for no rotation; else positions: int32 [tokens] (device).
+ * head_dim is a multiple of 16 up to 256.  BF16 rows that are contiguous may
+ * be rewritten in place. */
+int eq_qk_norm_rope(const void *q, uint64_t q_stride, uint32_t q_heads, const uint16_t *q_weight,
+                    uint16_t *q_out, const void *k, uint64_t k_stride, uint32_t k_heads,
+                    const uint16_t *k_weight, uint16_t *k_out, uint32_t dtype, uint32_t tokens,
+                    uint32_t head_dim, float eps, const int32_t *positions, const eq_rope *rope,
+                    hipStream_t stream);
+
+/* Bytes of a page; 0 if the sizes are not supported. */
+size_t eq_kv_page_bytes(uint32_t kv_heads, uint32_t head_dim, uint32_t page_tokens);
+
+/* Append a batch's rows to the cache: k and v are n_tokens rows of kv_heads x
+ * head_dim elements of `dtype`, k_stride and v_stride elements apart.  With
+ * rope, keys are rotated on the way, at positions[row] or, when that is NULL,
+ * at their place in the sequence; the rotation is in fp32 (each product and
+ * the sum rounded) and the result is rounded once, to its code.  Other tokens
+ * of the pages keep their values.  Two sequences of one call may share pages,
+ * but not 8 consecutive tokens that either appends to. */
+int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, const void *k,
+                 uint64_t k_stride, const void *v, uint64_t v_stride, uint32_t dtype,
+                 const int32_t *positions, const eq_rope *rope, hipStream_t stream);
+
+/* The values that the cache holds for a batch's rows, as BF16 (exact), to k
+ * and v: contiguous [n_tokens][kv_heads][head_dim], 16-byte aligned.  With
+ * seq_start the running sum of kv_len, whole sequences. */
+int eq_kv_read(const eq_kv_cache *cache, const eq_kv_batch *batch, uint16_t *k, uint16_t *v,
+               hipStream_t stream);
+
+/* Workspace bytes of eq_attn_kv4 (0 when it needs none, or on bad arguments). */
+size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
+                                   uint32_t q_heads);
+
+/* Attention over the cache: out[row][h] = sum_t P_t V_t / sum_t P_t with P_t =
+ * exp(scale q[row][h] . K_t - max), over the cached tokens t of the row's
+ * sequence up to its own position, and with window > 0 only the last `window`
+ * of them; zeros where there are none.  Query head h reads key/value head h /
+ * (q_heads / kv_heads).  q: BF16, n_tokens rows of q_heads x head_dim, q_stride
+ * elements apart, 16-byte aligned rows; out: BF16, contiguous, 16-byte
+ * aligned.  The new tokens' keys and values are in the cache already
+ * (eq_kv_append first).  scale > 0.  Scores, softmax statistics and sums are in
+ * fp32; queries enter exactly (down to 2^-18 of the largest of their 32
+ * channels), P with 8 significant bits.  A query with an infinity or NaN, and
+ * one that sees such a key or value, gives NaN.  ws/ws_bytes: at least
+ * eq_attn_kv4_workspace_bytes(), 16-byte aligned; nothing in it is kept
+ * between calls.  Sums are added in a fixed order. */
+int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
+                uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window, uint16_t *out,
+                void *ws, size_t ws_bytes, hipStream_t stream);
+
 /* Wait for `stream`, then report EQ_ECORRUPT if any decode since the last
  * eq_layer_prepare found a chunk whose stream or terminal states did not
  * check out, else EQ_OK (or EQ_EHIP). */

@@ -42,6 +42,23 @@ class eq_layer(ctypes.Structure):
                 ("n_singles", ctypes.c_uint32), ("row_order", _vp)]
 
 
+class eq_kv_cache(ctypes.Structure):
+    _fields_ = [("pages", _vp), ("n_pages", ctypes.c_uint32), ("page_tokens", ctypes.c_uint32),
+                ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32)]
+
+
+class eq_kv_batch(ctypes.Structure):
+    _fields_ = [("seq_start", _vp), ("kv_len", _vp), ("page_table", _vp),
+                ("n_seqs", ctypes.c_uint32), ("max_pages", ctypes.c_uint32),
+                ("n_tokens", ctypes.c_uint32), ("max_new", ctypes.c_uint32),
+                ("max_len", ctypes.c_uint32)]
+
+
+class eq_rope(ctypes.Structure):
+    _fields_ = [("cos", _vp), ("sin", _vp), ("rows", ctypes.c_uint32), ("dims", ctypes.c_uint32),
+                ("pairs", ctypes.c_uint32)]
+
+
 class eqe_params(ctypes.Structure):
     _fields_ = [("prob_bits", ctypes.c_uint32), ("chunk_syms", ctypes.c_uint32),
                 ("lanes", ctypes.c_uint32), ("threads", ctypes.c_uint32),
@@ -86,6 +103,17 @@ SIGNATURES = {
                                      _vp, ctypes.c_size_t, _vp]),
     "eq_decode_gemm": (ctypes.c_int, [ctypes.POINTER(eq_layer), _vp, ctypes.c_uint32, _vp, _vp,
                                       _vp, ctypes.c_size_t, _vp]),
+    "eq_qk_norm_rope": (ctypes.c_int, [_vp, ctypes.c_uint64, ctypes.c_uint32, _vp, _vp,
+                                       _vp, ctypes.c_uint64, ctypes.c_uint32, _vp, _vp,
+                                       ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32,
+                                       ctypes.c_float, _vp, _vp, _vp]),
+    "eq_kv_page_bytes": (ctypes.c_size_t, [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32]),
+    "eq_kv_append": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, _vp, ctypes.c_uint64,
+                                    ctypes.c_uint32, _vp, _vp, _vp]),
+    "eq_kv_read": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp]),
+    "eq_attn_kv4_workspace_bytes": (ctypes.c_size_t, [_vp, _vp, ctypes.c_uint32]),
+    "eq_attn_kv4": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_float,
+                                   ctypes.c_uint32, _vp, _vp, ctypes.c_size_t, _vp]),
     "eq_get_status": (ctypes.c_int, [ctypes.POINTER(eq_layer), _vp]),
     "eq_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "eqe_alpha_search": (ctypes.c_float, [_vp, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_double,
@@ -347,6 +375,187 @@ def eq_decode_gemm(L, x, B: int, bias, y, ws, stream=None) -> None:
 
 def eq_get_status(L, stream=None) -> int:
     return lib().eq_get_status(ctypes.byref(_raw(L)), _stream(stream))
+
+
+# ------------------------------------------------- 4-bit key/value cache ABI
+class Rope:
+    """Rotation by tables cos and sin [rows, dims / 2] (fp32, contiguous):
+    channels (c, c + dims/2) turn together, or with pairs (2c, 2c + 1)."""
+
+    def __init__(self, cos, sin, pairs: bool = False):
+        import torch
+        if cos.dim() != 2 or cos.shape != sin.shape:
+            raise ValueError("cos and sin are two [rows, dims / 2] tables")
+        self.tables = (cos, sin)
+        self.device = cos.device
+        self.raw = eq_rope(_dptr(cos, torch.float32), _dptr(sin, torch.float32), cos.shape[0],
+                           2 * cos.shape[1], int(bool(pairs)))
+        self.ptr = ctypes.addressof(self.raw)
+
+
+class KvCache:
+    """A paged cache of 4-bit keys and values in `pages` (uint8, n_pages x
+    eq_kv_page_bytes(), any shape with the pages in order)."""
+
+    def __init__(self, pages, *, page_tokens: int, kv_heads: int, head_dim: int):
+        import torch
+        nbytes = eq_kv_page_bytes(kv_heads, head_dim, page_tokens)
+        if nbytes == 0:
+            raise ValueError("unsupported cache: page_tokens a power of two from 32 to 4096, "
+                             "kv_heads up to 1024, head_dim 64 or 128")
+        ptr = _dptr(pages, torch.uint8)
+        if pages.numel() == 0 or pages.numel() % nbytes:
+            raise ValueError(f"pages holds {pages.numel()} bytes, not a multiple of {nbytes}")
+        self.pages, self.page_bytes = pages, nbytes
+        self.device = pages.device
+        self.raw = eq_kv_cache(ptr, pages.numel() // nbytes, page_tokens, kv_heads, head_dim)
+        self.ptr = ctypes.addressof(self.raw)
+        self.kv_heads, self.head_dim = kv_heads, head_dim
+
+    @classmethod
+    def empty(cls, n_pages: int, *, page_tokens: int, kv_heads: int, head_dim: int, device="cuda"):
+        import torch
+        pages = torch.empty(n_pages, eq_kv_page_bytes(kv_heads, head_dim, page_tokens),
+                            dtype=torch.uint8, device=device)
+        return cls(pages, page_tokens=page_tokens, kv_heads=kv_heads, head_dim=head_dim)
+
+
+class KvBatch:
+    """The tokens of a call (eq_kv_batch): seq_start [n + 1], kv_len [n] and
+    page_table [n, max_pages], int32 on the device and read there, so their
+    contents may change between calls; n_tokens, max_new and max_len bound
+    them."""
+
+    def __init__(self, seq_start, kv_len, page_table, *, n_tokens: int, max_new: int,
+                 max_len: int):
+        import torch
+        n = kv_len.numel()
+        if seq_start.numel() != n + 1 or page_table.dim() != 2 or page_table.shape[0] != n:
+            raise ValueError("seq_start has n + 1 entries, kv_len n, page_table n rows")
+        if not kv_len.device == seq_start.device == page_table.device:
+            raise ValueError("the batch's tensors are on several devices")
+        if min(n_tokens, max_new, max_len) < 0:
+            raise ValueError("negative bound")
+        self.tensors = (seq_start, kv_len, page_table)
+        self.device = kv_len.device
+        self.raw = eq_kv_batch(_dptr(seq_start, torch.int32), _dptr(kv_len, torch.int32),
+                               _dptr(page_table, torch.int32), n, page_table.shape[1], n_tokens,
+                               max_new, max_len)
+        self.ptr = ctypes.addressof(self.raw)
+        self.n_tokens = n_tokens
+
+
+_KINDS = None  # torch dtype -> EQ_F32 or EQ_BF16
+
+
+def _head_rows(x, heads, head_dim, what):
+    """(pointer, token stride, element type) of x [tokens, heads, head_dim],
+    whose tokens may be apart and whose heads lie one after another."""
+    global _KINDS
+    if _KINDS is None:
+        import torch
+        _KINDS = {torch.float32: 0, torch.bfloat16: 1}
+    kind = _KINDS.get(x.dtype)
+    if kind is None:
+        raise ValueError(f"{what}: expected float32 or bfloat16, got {x.dtype}")
+    if not x.is_cuda or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim:
+        raise ValueError(f"{what}: expected a device tensor [tokens, {heads}, {head_dim}]")
+    st = x.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != head_dim) or st[0] < 0:
+        raise ValueError(f"{what}: the heads of a token have to be contiguous")
+    return x.data_ptr(), st[0] if x.shape[0] > 1 else heads * head_dim, kind
+
+
+def _bf16_out(t, numel, what):
+    import torch
+    if t.dtype is not torch.bfloat16 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous bfloat16 device tensor")
+    if t.numel() < numel:
+        raise ValueError(f"{what}: tensor too small: {t.numel()} < {numel}")
+    return t.data_ptr()
+
+
+def eq_qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: float = 1e-6,
+                    rope=None, positions=None, stream=None) -> None:
+    """Norm of each head of q and k [tokens, heads, head_dim] (fp32 or BF16;
+    k may be None) and its rotation, to BF16: q_out, k_out contiguous."""
+    import torch
+    tokens, heads, dim = q.shape
+    pq, sq, kind = _head_rows(q, heads, dim, "q")
+    pqo = _bf16_out(q_out, tokens * heads * dim, "q_out")
+    pk = pko = None
+    sk = hk = 0
+    if k is not None:
+        hk = k.shape[1]
+        if k.shape[0] != tokens or k.dtype != q.dtype:
+            raise ValueError("q and k differ in tokens or type")
+        pk, sk, _ = _head_rows(k, hk, dim, "k")
+        pko = _bf16_out(k_out, tokens * hk * dim, "k_out")
+    pqw = _dptr(q_weight, torch.bfloat16, dim)
+    pkw = _dptr(k_weight, torch.bfloat16, dim)
+    if rope is not None and positions is None:
+        raise ValueError("a rotation needs positions")
+    pp = _dptr(positions, torch.int32, tokens)
+    _check("eq_qk_norm_rope",
+           lib().eq_qk_norm_rope(pq, sq, heads, pqw, pqo, pk, sk, hk, pkw, pko, kind, tokens, dim,
+                                 eps, pp, None if rope is None else rope.ptr, _stream(stream)))
+
+
+def eq_kv_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    return lib().eq_kv_page_bytes(kv_heads, head_dim, page_tokens)
+
+
+def eq_kv_append(cache, batch, k, v, *, rope=None, positions=None, stream=None) -> None:
+    """Append k and v [n_tokens, kv_heads, head_dim] (fp32 or BF16), the keys
+    rotated on the way when rope is given: at `positions`, or at the tokens'
+    places in their sequences."""
+    import torch
+    pk, sk, kind = _head_rows(k, cache.kv_heads, cache.head_dim, "k")
+    pv, sv, kind_v = _head_rows(v, cache.kv_heads, cache.head_dim, "v")
+    if kind != kind_v:
+        raise ValueError("k and v differ in type")
+    if k.shape[0] < batch.n_tokens or v.shape[0] < batch.n_tokens:
+        raise ValueError("fewer rows than the batch's tokens")
+    pp = _dptr(positions, torch.int32, batch.n_tokens)
+    _check("eq_kv_append",
+           lib().eq_kv_append(cache.ptr, batch.ptr, pk, sk, pv, sv, kind, pp,
+                              None if rope is None else rope.ptr, _stream(stream)))
+
+
+def eq_kv_read(cache, batch, k, v, stream=None) -> None:
+    """The cache's values of the batch's tokens, as BF16: k and v contiguous
+    [n_tokens, kv_heads, head_dim]."""
+    n = batch.n_tokens * cache.kv_heads * cache.head_dim
+    _check("eq_kv_read", lib().eq_kv_read(cache.ptr, batch.ptr, _bf16_out(k, n, "k"),
+                                          _bf16_out(v, n, "v"), _stream(stream)))
+
+
+def eq_attn_kv4_workspace_bytes(cache, batch, q_heads: int) -> int:
+    return lib().eq_attn_kv4_workspace_bytes(cache.ptr, batch.ptr, q_heads)
+
+
+def attn_workspace(cache, batch, q_heads: int):
+    """A device workspace for eq_attn_kv4 (None when it needs none)."""
+    import torch
+    n = eq_attn_kv4_workspace_bytes(cache, batch, q_heads)
+    return torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
+
+
+def eq_attn_kv4(cache, batch, q, scale: float, out, ws=None, *, window: int = 0,
+                stream=None) -> None:
+    """Causal attention of q [n_tokens, q_heads, head_dim] (BF16) over the
+    cache to out (BF16, contiguous); with window, over the last `window`
+    positions only."""
+    heads = q.shape[1]
+    pq, sq, kind = _head_rows(q, heads, cache.head_dim, "q")
+    if kind != 1:
+        raise ValueError("q: expected bfloat16")
+    if q.shape[0] < batch.n_tokens:
+        raise ValueError("fewer rows than the batch's tokens")
+    po = _bf16_out(out, batch.n_tokens * heads * cache.head_dim, "out")
+    pw, nbytes = (None, 0) if ws is None else (_dptr(ws), ws.numel() * ws.element_size())
+    _check("eq_attn_kv4", lib().eq_attn_kv4(cache.ptr, batch.ptr, pq, sq, heads, scale, window, po,
+                                            pw, nbytes, _stream(stream)))
 
 
 # ---------------------------------------------------------------- encoder ABI

@@ -33,7 +33,8 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(BUILD, src + ".o")
         _run(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    for src in ("eq_decode.hip", "eq_decode2.hip", "eq_gemm.hip"):
+    for src in ("eq_decode.hip", "eq_decode2.hip", "eq_gemm.hip", "eq_kv.hip",
+                "eq_attn.hip"):
         obj = os.path.join(BUILD, src + ".o")
         _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)

@@ -1,0 +1,543 @@
+// Attention over the 4-bit key/value cache (declared in include/eq.h).
+//
+// For one key/value head the queries that read it (its query heads at every
+// new token of a sequence) are columns, cached tokens are rows:
+//   S = K q^T,  P = exp2(c S - m),  O = V^T (w P),  out = O / sum P
+// with c = scale log2 e, m the running maximum of a column and w_t the scale of
+// token t's value.  Both products run on the scaled matrix instructions, which
+// take E2M1 codes with one power-of-two scale for 32 of them as they lie in the
+// cache, so neither keys nor values are ever decoded.  The other operand has to
+// be 8 bits wide: q and w P enter as the sum of two E4M3 numbers, x = h + l with
+// h = e4m3(x) and l = e4m3(x - h), 4 significant bits each.  That holds all of a
+// BF16 query, and w P to 8 significant bits, with a relative error below 2^-8 in
+// each term and no bias.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "eq.h"
+#include "eq_device.h"
+#include "eq_kv.h"
+
+namespace {
+
+using namespace eq_kv;
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef int int8v __attribute__((ext_vector_type(8)));
+typedef short short2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t kTile = 128;  // tokens a wavefront takes at a time
+constexpr uint32_t kCols = 16;   // query columns of a block
+constexpr uint32_t kWaves = 4;
+constexpr int kUnitScale = 127;  // scale byte of 1
+
+struct AttnArgs {
+  View w;
+  const uint16_t *q;
+  uint64_t q_stride;
+  uint16_t *out;
+  float *part;       // [n_seqs][kv_heads][q_tiles][chunks][kCols][D] sums of a chunk
+  float2 *stat;      // the same without D: maximum and sum of P
+  uint32_t group;    // query heads of a key/value head
+  uint32_t window;
+  uint32_t q_tiles, chunks, chunk_tiles;
+  float c;           // scale log2 e
+};
+
+// Columns [col0, col0 + kCols) of a sequence, and the cached tokens they see.
+struct Span {
+  uint32_t cols;          // columns of the sequence
+  uint32_t first, last;   // token tiles [first, last)
+  uint32_t chunks;
+  int32_t hi_min, lo_max; // tokens in [lo_max, hi_min) are seen by every column
+};
+
+__device__ inline int32_t end_of(const Seq &q, int32_t pos) { return max(min(pos + 1, q.len), 0); }
+__device__ inline int32_t start_of(uint32_t window, int32_t pos) {
+  return window && pos >= 0 && uint32_t(pos) >= window ? pos + 1 - int32_t(window) : 0;
+}
+
+__device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
+  Span p{};
+  p.cols = uint32_t(q.count) * a.group;
+  if (col0 >= p.cols) return p;
+  const int32_t pos0 = q.base + int32_t(col0 / a.group);
+  const int32_t pos1 = q.base + int32_t((min(col0 + kCols, p.cols) - 1) / a.group);
+  p.hi_min = end_of(q, pos0);
+  p.lo_max = start_of(a.window, pos1);
+  const uint32_t lo = uint32_t(start_of(a.window, pos0)), hi = uint32_t(end_of(q, pos1));
+  p.first = lo / kTile;
+  p.last = max((hi + kTile - 1) / kTile, p.first);
+  p.chunks = (p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles;
+  return p;
+}
+
+// x / scale as two E4M3 terms, of four values: h at `scale`, l at scale / 16.
+__device__ inline void split4(const float *x, float scale, int &h, int &l) {
+  short2v a = {0, 0}, b = {0, 0};
+  a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, x[0], x[1], scale, false);
+  a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, x[2], x[3], scale, true);
+  h = __builtin_bit_cast(int, a);
+  const float2v u = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, scale, false);
+  const float2v v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, scale, true);
+  const float s = scale * 0.0625f;
+  b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, x[0] - u[0], x[1] - u[1], s, false);
+  b = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(b, x[2] - v[0], x[3] - v[1], s, true);
+  l = __builtin_bit_cast(int, b);
+}
+
+// Scale byte that brings magnitudes of the exponent of `top` to [128, 256);
+// 255 for an infinity or NaN.  Its lower term's byte is 4 less.
+__device__ inline int top_byte(uint32_t top) {
+  const int e = int(top >> 23);
+  return e == 255 ? 255 : max(e - 7, 8);
+}
+__device__ inline int low_byte(int b) { return b == 255 ? 255 : b - 4; }
+__device__ inline float byte_value(int b) { return __uint_as_float(uint32_t(b) << 23); }
+
+__device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The query columns as the second operand of the key product.  Lane (col, g)
+// holds channels 16 g .. of the first half of the operand's 128 steps and 16 g ..
+// of the second, and lane group b the scale of steps 32 b ..  At D = 128 the
+// steps are the channels, and the two terms are two operands; at D = 64 the
+// halves are the two terms, met by the same keys twice.
+template <int D>
+struct Query {
+  int8v h, l;
+  int hs, ls;
+  __device__ inline void load(const uint16_t *row, uint32_t col, uint32_t g) {
+    float x[32];
+    auto half = [&](int at, uint32_t ch) {
+      uint32_t u[8] = {};
+      if (row) {
+        *reinterpret_cast<uint4 *>(u) = *reinterpret_cast<const uint4 *>(row + ch);
+        *reinterpret_cast<uint4 *>(u + 4) = *reinterpret_cast<const uint4 *>(row + ch + 8);
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[at + 2 * i] = __uint_as_float(u[i] << 16);
+        x[at + 2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        top = max(top, max(u[i] << 16 & 0x7FFFFFFFu, u[i] & 0x7FFF0000u));
+      }
+      return top_byte(max(top, uint32_t(__shfl_xor(int(top), 16))));
+    };
+    const int a = half(0, 16 * g);
+    const int from_a = __shfl(a, int(32 * (g & 1) + col));
+    if constexpr (D == 128) {
+      const int b = half(16, 64 + 16 * g);
+      const int from_b = __shfl(b, int(32 * (g & 1) + col));
+      hs = g < 2 ? from_a : from_b;
+      ls = low_byte(hs);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        int u, v;
+        split4(x + 4 * i, byte_value(i < 4 ? a : b), u, v);
+        h[i] = u;
+        l[i] = v;
+      }
+    } else {
+      hs = g < 2 ? from_a : low_byte(from_a);
+      ls = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int u, v;
+        split4(x + 4 * i, byte_value(a), u, v);
+        h[i] = u;
+        h[4 + i] = v;
+      }
+    }
+  }
+};
+
+__device__ inline int8v widen(int4v v) { return int8v{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
+
+// One block: kCols query columns of a key/value head against a chunk of token
+// tiles, dealt to its 4 wavefronts in turn; each keeps its own maximum, sum and
+// O, joined through LDS at the end.
+//
+// Layout.  The product of 16 tokens leaves lane (col, g) with rows 4 g + r, r =
+// 0..3, of its column; the second product wants w P in lane (col, g) for steps
+// 16 g .. + 15 and 64 + 16 g .. + 15.  Which token a row is, is free: row 4 g +
+// r of product i (0..7) is token 64 (i / 4) + 16 g + 4 (i % 4) + r of the tile.
+// Then a lane's 32 scores are the 32 tokens of its steps in order, and P passes
+// from the first product to the second without leaving the lane.  V lies along
+// the tokens in the cache, 32 to a 16-byte row, as the second product takes it.
+template <int D, bool ONE>
+__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
+  constexpr int ND = D / 16;
+  constexpr uint32_t kStride = D + 4;  // floats a column in LDS
+  __shared__ __attribute__((aligned(16))) float lds_o[kWaves * kCols * kStride];
+  __shared__ float2 lds_s[kWaves][kCols];
+  const View &w = a.w;
+  const uint32_t s = blockIdx.y;
+  const uint32_t chunk = blockIdx.x % a.chunks, rest = blockIdx.x / a.chunks;
+  const uint32_t qt = rest % a.q_tiles, h = rest / a.q_tiles;
+  const Seq q = sequence(w, s);
+  const uint32_t col0 = qt * kCols;
+  const Span sp = span_of(a, q, col0);
+  if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
+  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t col = lane & 15, g = lane >> 4;
+
+  // this lane's column
+  const uint32_t index = col0 + col;
+  const bool real = index < sp.cols;
+  const uint32_t token = index / a.group;
+  const int32_t pos = q.base + int32_t(token);
+  const int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
+  Query<D> query;
+  query.load(real ? a.q + uint64_t(q.row + token) * a.q_stride +
+                        uint64_t(h * a.group + index % a.group) * D
+                  : nullptr,
+             col, g);
+
+  const uint32_t t_end = min(sp.first + (chunk + 1) * a.chunk_tiles, sp.last);
+  uint32_t t = sp.first + chunk * a.chunk_tiles + wave;
+
+  // addresses: the four 32-token units of a tile may be in four pages
+  const int32_t *const table = w.page_table + size_t(s) * w.max_pages;
+  const uint32_t seen = uint32_t(end_of(q, q.base + int32_t((min(col0 + kCols, sp.cols) - 1) / a.group)));
+  const uint32_t last_unit = seen ? (seen - 1) / kUnit : 0;
+  const uint32_t page_mask = (1u << w.page_shift) - 1;
+  const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
+  auto first_token = [&](uint32_t tile, uint32_t unit) {
+    return min(tile * 4 + unit, last_unit) * kUnit;
+  };
+  struct Ids {
+    int ka, kb, v, sa, sb;
+  };
+  const uint32_t gk = (lane & 15) >> 2, r = lane & 3;
+  auto load_ids = [&](uint32_t tile) {
+    Ids d;
+    if constexpr (ONE) {
+      d.ka = table[first_token(tile, 0) >> w.page_shift];
+      d.kb = d.v = d.sa = d.sb = d.ka;
+    } else {
+      d.ka = table[first_token(tile, gk >> 1) >> w.page_shift];
+      d.kb = table[first_token(tile, 2 + (gk >> 1)) >> w.page_shift];
+      d.v = table[first_token(tile, g) >> w.page_shift];
+      d.sa = table[first_token(tile, g >> 1) >> w.page_shift];
+      d.sb = table[first_token(tile, 2 + (g >> 1)) >> w.page_shift];
+    }
+    return d;
+  };
+  auto part_of = [&](int id) {
+    return base + (uint32_t(id) < w.n_pages ? uint64_t(uint32_t(id)) : 0) * w.page_bytes;
+  };
+  auto slot_of = [&](uint32_t tile, uint32_t unit) { return first_token(tile, unit) & page_mask; };
+
+  int4v kreg[8], vreg[ND];
+  uint4 va, vb;
+  int ksa, ksb;
+  const uint32_t kg = D == 128 ? g : g & 1;
+  auto load_k = [&](uint32_t tile, const Ids &d) {
+    const uint8_t *const pa = part_of(d.ka), *const pb = part_of(d.kb);
+    const uint32_t a0 = slot_of(tile, gk >> 1) + 16 * (gk & 1);
+    const uint32_t b0 = slot_of(tile, 2 + (gk >> 1)) + 16 * (gk & 1);
+    const uint8_t *const ra = pa + (a0 + r) * (D / 2) + 16 * kg;
+    const uint8_t *const rb = pb + (b0 + r) * (D / 2) + 16 * kg;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      kreg[i] = *reinterpret_cast<const int4v *>(ra + i * 2 * D);
+      kreg[4 + i] = *reinterpret_cast<const int4v *>(rb + i * 2 * D);
+    }
+    ksa = *reinterpret_cast<const int *>(pa + w.ks_off + a0 / 16 * (D / 2) + (r * (D / 32) + kg) * 4);
+    ksb = *reinterpret_cast<const int *>(pb + w.ks_off + b0 / 16 * (D / 2) + (r * (D / 32) + kg) * 4);
+  };
+  auto load_vs = [&](uint32_t tile, const Ids &d) {
+    va = *reinterpret_cast<const uint4 *>(part_of(d.sa) + w.vs_off + slot_of(tile, g >> 1) +
+                                          16 * (g & 1));
+    vb = *reinterpret_cast<const uint4 *>(part_of(d.sb) + w.vs_off + slot_of(tile, 2 + (g >> 1)) +
+                                          16 * (g & 1));
+  };
+  auto load_v = [&](uint32_t tile, const Ids &d) {
+    const uint8_t *const p = part_of(d.v) + w.v_off +
+                             (slot_of(tile, g) / kUnit * D + (lane & 15)) * 16;
+#pragma unroll
+    for (int m = 0; m < ND; ++m) vreg[m] = *reinterpret_cast<const int4v *>(p + m * 256);
+  };
+
+  float m_run = -INFINITY, l_run = 0.0f;
+  floatx4 o[ND];
+#pragma unroll
+  for (int m = 0; m < ND; ++m) o[m] = floatx4{0, 0, 0, 0};
+
+  Ids cur{}, next{};
+  if (t < t_end) {
+    cur = load_ids(t);
+    next = load_ids(t + kWaves);
+    load_k(t, cur);
+    load_vs(t, cur);
+    load_v(t, cur);
+  }
+  for (; t < t_end; t += kWaves) {
+    const bool more = t + kWaves < t_end;
+    floatx4 sc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int8v k8 = widen(kreg[i]);
+      const int ks = i < 4 ? ksa : ksb;
+      sc[i] = floatx4{0, 0, 0, 0};
+      auto mul = [&](int8v b, int bs) {
+        switch (i & 3) {
+          case 0: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 0, ks, 0, bs); break;
+          case 1: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 1, ks, 0, bs); break;
+          case 2: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 2, ks, 0, bs); break;
+          default: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 3, ks, 0, bs); break;
+        }
+      };
+      mul(query.h, query.hs);
+      if constexpr (D == 128) mul(query.l, query.ls);
+    }
+    const bool bad_a = uint32_t(cur.sa) >= w.n_pages, bad_b = uint32_t(cur.sb) >= w.n_pages;
+    Ids after = next;
+    if (more) {
+      after = load_ids(t + 2 * kWaves);
+      load_k(t + kWaves, next);
+    }
+    // masks, only where some column does not see the whole tile
+    const int32_t at = int32_t(t * kTile);
+    uint32_t visible = ~0u;  // bit 4 i + r: this lane's column sees that token
+    if (at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || __any(bad_a || bad_b)) {
+      visible = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int32_t tok = at + 64 * (i / 4) + 16 * int32_t(g) + 4 * (i % 4) + e;
+          const bool ok = tok >= lo && tok < hi && !(i < 4 ? bad_a : bad_b);
+          visible |= uint32_t(ok) << (4 * i + e);
+          if (!ok) sc[i][e] = -INFINITY;
+        }
+    }
+    float mx = sc[0][0];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[i][e]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float m_new = fmaxf(m_run, mx * a.c);
+    const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+    if (__any(m_new > m_run)) {
+      const float f = exp2_(m_run - m_use);
+      l_run *= f;
+#pragma unroll
+      for (int m = 0; m < ND; ++m) o[m] *= f;
+      m_run = m_new;
+    }
+    float y[32];
+    float top = 0.0f;
+    const uint32_t vs[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p = exp2_(__builtin_fmaf(sc[i][e], a.c, -m_use));
+        l_run += p;
+        y[4 * i + e] = p * __uint_as_float((vs[i] >> (8 * e) & 255u) << 23);
+      }
+    if (visible != ~0u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!(visible >> i & 1)) y[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
+    if (more) load_vs(t + kWaves, next);
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const int ps = top_byte(__float_as_uint(top));
+    const int pl = low_byte(ps);
+    const float scale = byte_value(ps);
+    int8v ph, pq;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      int u, v;
+      split4(y + 4 * i, scale, u, v);
+      ph[i] = u;
+      pq[i] = v;
+    }
+#pragma unroll
+    for (int m = 0; m < ND; ++m) {
+      const int8v v8 = widen(vreg[m]);
+      o[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8, ph, o[m], 4, 0, 0, kUnitScale, 0, ps);
+      o[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8, pq, o[m], 4, 0, 0, kUnitScale, 0, pl);
+    }
+    if (more) load_v(t + kWaves, next);
+    cur = next;
+    next = after;
+  }
+  l_run += __shfl_xor(l_run, 16);
+  l_run += __shfl_xor(l_run, 32);
+
+  // join the wavefronts: column c of wave v at lds_o[(v kCols + c) kStride]
+  if (g == 0) lds_s[wave][col] = make_float2(m_run, l_run);
+#pragma unroll
+  for (int m = 0; m < ND; ++m)
+    *reinterpret_cast<floatx4 *>(lds_o + (wave * kCols + col) * kStride + 16 * m + 4 * g) = o[m];
+  __syncthreads();
+  constexpr uint32_t kPer = D * kCols / 256;  // channels a thread
+  const uint32_t oc = threadIdx.x / (256 / kCols), d0 = threadIdx.x % (256 / kCols) * kPer;
+  if (col0 + oc >= sp.cols) return;
+  float m_all = -INFINITY, l_all = 0.0f, sum[kPer] = {};
+#pragma unroll
+  for (uint32_t v = 0; v < kWaves; ++v) m_all = fmaxf(m_all, lds_s[v][oc].x);
+  const float m_use = m_all == -INFINITY ? 0.0f : m_all;
+#pragma unroll
+  for (uint32_t v = 0; v < kWaves; ++v) {
+    const float f = exp2_(lds_s[v][oc].x - m_use);
+    l_all += f * lds_s[v][oc].y;
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) sum[i] += f * lds_o[(v * kCols + oc) * kStride + d0 + i];
+  }
+  if (sp.chunks <= 1) {
+    const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
+    const uint32_t i0 = col0 + oc;
+    uint32_t pk[kPer / 2];
+#pragma unroll
+    for (uint32_t i = 0; i < kPer / 2; ++i)
+      pk[i] = eq_dev::pack_bf16(sum[2 * i] * inv, sum[2 * i + 1] * inv);
+    uint16_t *const out = a.out + (uint64_t(q.row + i0 / a.group) * w.kv_heads * a.group +
+                                   h * a.group + i0 % a.group) * D + d0;
+#pragma unroll
+    for (uint32_t i = 0; i < kPer / 2; ++i) reinterpret_cast<uint32_t *>(out)[i] = pk[i];
+    return;
+  }
+  const uint64_t slot = (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks + chunk) * kCols + oc;
+  if (d0 == 0) a.stat[slot] = make_float2(m_all, l_all);
+#pragma unroll
+  for (uint32_t i = 0; i < kPer; ++i) a.part[slot * D + d0 + i] = sum[i];
+}
+
+// Joins the chunks of one query head at one new token, a block each: 8
+// sub-blocks of threads take the chunks in turn, then add up through LDS.
+template <int D>
+__global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
+  constexpr uint32_t kLanes = D / 4, kSub = 8;
+  __shared__ __attribute__((aligned(16))) float4 lds[kSub][kLanes];
+  __shared__ float lds_l[kSub];
+  const View &w = a.w;
+  const uint32_t s = blockIdx.y, heads = w.kv_heads * a.group;
+  const uint32_t token = blockIdx.x / heads, head = blockIdx.x % heads;
+  const Seq q = sequence(w, s);
+  if (int32_t(token) >= q.count) return;
+  const uint32_t h = head / a.group, index = token * a.group + head % a.group;
+  const uint32_t qt = index / kCols;
+  const Span sp = span_of(a, q, qt * kCols);
+  if (sp.chunks <= 1) return;
+  const uint64_t first = (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * kCols + index % kCols;
+  float m = -INFINITY;
+  for (uint32_t c = 0; c < sp.chunks; ++c) m = fmaxf(m, a.stat[first + uint64_t(c) * kCols].x);
+  if (m == -INFINITY) m = 0.0f;
+  const uint32_t sub = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
+  float4 o = make_float4(0, 0, 0, 0);
+  float total = 0.0f;
+#pragma unroll 4
+  for (uint32_t c = sub; c < sp.chunks; c += kSub) {
+    const uint64_t at = first + uint64_t(c) * kCols;
+    const float2 st = a.stat[at];
+    const float4 x = *reinterpret_cast<const float4 *>(a.part + at * D + 4 * l);
+    const float f = exp2_(st.x - m);
+    total += f * st.y;
+    o.x += f * x.x, o.y += f * x.y, o.z += f * x.z, o.w += f * x.w;
+  }
+  lds[sub][l] = o;
+  if (l == 0) lds_l[sub] = total;
+  __syncthreads();
+  if (sub) return;
+#pragma unroll
+  for (uint32_t i = 1; i < kSub; ++i) {
+    const float4 x = lds[i][l];
+    o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+    total += lds_l[i];
+  }
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  *reinterpret_cast<uint2 *>(a.out + (uint64_t(q.row + token) * heads + head) * D + 4 * l) =
+      make_uint2(eq_dev::pack_bf16(o.x * inv, o.y * inv), eq_dev::pack_bf16(o.z * inv, o.w * inv));
+}
+
+// How a call is launched: chunks of token tiles so that the blocks fill the
+// card about twice over, none shorter than a tile for each wavefront, and up to
+// 2048 query tiles none longer than 32 tiles (a ragged batch's longest sequence
+// then spreads over the card too).
+struct Plan {
+  uint32_t q_tiles, chunks, chunk_tiles;
+};
+
+Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_new,
+               uint32_t max_len) {
+  Plan p;
+  p.q_tiles = uint32_t((uint64_t(max_new) * group + kCols - 1) / kCols);
+  const uint64_t work = uint64_t(n_seqs) * kv_heads * p.q_tiles;
+  const uint32_t tiles = (max_len + kTile - 1) / kTile;
+  const uint64_t want = std::max<uint64_t>(1, (512 + work - 1) / work);
+  uint32_t ct = uint32_t((tiles + want - 1) / want);
+  ct = std::max((ct + kWaves - 1) / kWaves * kWaves, kWaves);
+  if (work <= 2048) ct = std::min(ct, 32u);
+  p.chunk_tiles = ct;
+  p.chunks = std::max((tiles + ct - 1) / ct, 1u);
+  return p;
+}
+
+size_t attn_bytes(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
+  if (p.chunks <= 1) return 0;
+  return size_t(b->n_seqs) * c->kv_heads * p.q_tiles * p.chunks * kCols * (c->head_dim + 2) *
+         sizeof(float);
+}
+
+bool heads_ok(const eq_kv_cache *c, uint32_t q_heads) {
+  return q_heads >= 1 && q_heads % c->kv_heads == 0 && q_heads <= 65535;
+}
+
+}  // namespace
+
+extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
+                                              uint32_t q_heads) {
+  if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || batch->n_seqs == 0 ||
+      batch->max_new == 0)
+    return 0;
+  return attn_bytes(plan_attn(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads,
+                              batch->max_new, batch->max_len),
+                    cache, batch);
+}
+
+extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
+                           uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
+                           uint16_t *out, void *ws, size_t ws_bytes, hipStream_t stream) {
+  if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || !(scale > 0.0f) || !std::isfinite(scale))
+    return EQ_EINVAL;
+  if (batch->n_seqs == 0 || batch->max_new == 0) return EQ_OK;
+  if (!q || !out || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15) ||
+      q_stride % 8 || (batch->n_tokens > 1 && q_stride < uint64_t(q_heads) * cache->head_dim))
+    return EQ_EINVAL;
+  const uint32_t group = q_heads / cache->kv_heads;
+  const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len);
+  const size_t need = attn_bytes(p, cache, batch);
+  if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return EQ_EINVAL;
+  const uint64_t blocks = uint64_t(cache->kv_heads) * p.q_tiles * p.chunks;
+  const uint64_t joins = uint64_t(batch->max_new) * q_heads;
+  if (blocks > 0x7FFFFFFFu || joins > 0x7FFFFFFFu) return EQ_EINVAL;
+  AttnArgs a{view(cache, batch), q, q_stride, out, static_cast<float *>(ws), nullptr, group, window,
+             p.q_tiles, p.chunks, p.chunk_tiles, scale * 1.44269504088896340736f};
+  if (need)
+    a.stat = reinterpret_cast<float2 *>(a.part + size_t(batch->n_seqs) * cache->kv_heads * p.q_tiles *
+                                                     p.chunks * kCols * cache->head_dim);
+  const dim3 grid(uint32_t(blocks), batch->n_seqs), join(uint32_t(joins), batch->n_seqs);
+  const bool one = cache->page_tokens >= kTile;
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
+  if (cache->head_dim == 128) {
+    one ? go(attn_kernel<128, true>) : go(attn_kernel<128, false>);
+    if (p.chunks > 1) hipLaunchKernelGGL(join_kernel<128>, join, dim3(256), 0, stream, a);
+  } else {
+    one ? go(attn_kernel<64, true>) : go(attn_kernel<64, false>);
+    if (p.chunks > 1) hipLaunchKernelGGL(join_kernel<64>, join, dim3(128), 0, stream, a);
+  }
+  return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP;
+}
