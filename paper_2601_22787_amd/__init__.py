@@ -445,33 +445,61 @@ class KvBatch:
         self.n_tokens = n_tokens
 
 
-_KINDS = None  # torch dtype -> EQ_F32 or EQ_BF16
+_KINDS = {}  # torch dtype -> EQ_F32 or EQ_BF16, filled by the first call
+_BF16 = _I32 = None
 
 
-def _head_rows(x, heads, head_dim, what):
-    """(pointer, token stride, element type) of x [tokens, heads, head_dim],
-    whose tokens may be apart and whose heads lie one after another."""
-    global _KINDS
-    if _KINDS is None:
-        import torch
-        _KINDS = {torch.float32: 0, torch.bfloat16: 1}
-    kind = _KINDS.get(x.dtype)
-    if kind is None:
-        raise ValueError(f"{what}: expected float32 or bfloat16, got {x.dtype}")
-    if not x.is_cuda or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim:
-        raise ValueError(f"{what}: expected a device tensor [tokens, {heads}, {head_dim}]")
-    st = x.stride()
-    if st[2] != 1 or (heads > 1 and st[1] != head_dim) or st[0] < 0:
-        raise ValueError(f"{what}: the heads of a token have to be contiguous")
-    return x.data_ptr(), st[0] if x.shape[0] > 1 else heads * head_dim, kind
-
-
-def _bf16_out(t, numel, what):
+def _kinds():
+    global _BF16, _I32
     import torch
-    if t.dtype is not torch.bfloat16 or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous bfloat16 device tensor")
-    if t.numel() < numel:
-        raise ValueError(f"{what}: tensor too small: {t.numel()} < {numel}")
+    _BF16, _I32 = torch.bfloat16, torch.int32
+    _KINDS.update({torch.float32: 0, torch.bfloat16: 1})
+
+
+def _head_rows(x, shape, what):
+    """(pointer, token stride, element type) of x [tokens, heads, head_dim],
+    whose tokens may be apart and whose heads lie one after another; shape:
+    x.shape.  (These checks are most of a small call's host time, hence one
+    look at each property.)"""
+    if not _KINDS:
+        _kinds()
+    kind = _KINDS.get(x.dtype)
+    tokens, heads, dim = shape
+    step, head, one = x.stride()
+    if kind is None or not x.is_cuda or one != 1 or (head != dim and heads > 1):
+        raise ValueError(f"{what}: expected float32 or bfloat16 [tokens, heads, head_dim] on the "
+                         "device, the heads of a token contiguous")
+    return x.data_ptr(), step if tokens > 1 else heads * dim, kind
+
+
+def _cache_rows(x, cache, batch, what):
+    """_head_rows of rows that go into the cache."""
+    shape = x.shape
+    if len(shape) != 3 or shape[1] != cache.kv_heads or shape[2] != cache.head_dim or \
+            shape[0] < batch.n_tokens:
+        raise ValueError(f"{what}: expected [{batch.n_tokens} tokens, {cache.kv_heads}, "
+                         f"{cache.head_dim}], got {tuple(shape)}")
+    return _head_rows(x, shape, what)
+
+
+def _bf16(t, numel, what):
+    """Pointer of a contiguous BF16 device tensor of at least numel elements, or None."""
+    if t is None:
+        return None
+    if not _KINDS:
+        _kinds()
+    if t.dtype is not _BF16 or not t.is_cuda or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{what}: expected a contiguous bfloat16 device tensor of at least "
+                         f"{numel} elements")
+    return t.data_ptr()
+
+
+def _positions(t, tokens):
+    if t is None:
+        return None
+    if t.dtype is not _I32 or not t.is_cuda or not t.is_contiguous() or t.numel() < tokens:
+        raise ValueError(f"positions: expected a contiguous int32 device tensor of at least "
+                         f"{tokens} elements")
     return t.data_ptr()
 
 
@@ -479,26 +507,29 @@ def eq_qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: fl
                     rope=None, positions=None, stream=None) -> None:
     """Norm of each head of q and k [tokens, heads, head_dim] (fp32 or BF16;
     k may be None) and its rotation, to BF16: q_out, k_out contiguous."""
-    import torch
-    tokens, heads, dim = q.shape
-    pq, sq, kind = _head_rows(q, heads, dim, "q")
-    pqo = _bf16_out(q_out, tokens * heads * dim, "q_out")
+    shape = q.shape
+    tokens, heads, dim = shape
+    pq, sq, kind = _head_rows(q, shape, "q")
+    pqo = _bf16(q_out, tokens * heads * dim, "q_out")
     pk = pko = None
     sk = hk = 0
     if k is not None:
-        hk = k.shape[1]
-        if k.shape[0] != tokens or k.dtype != q.dtype:
-            raise ValueError("q and k differ in tokens or type")
-        pk, sk, _ = _head_rows(k, hk, dim, "k")
-        pko = _bf16_out(k_out, tokens * hk * dim, "k_out")
-    pqw = _dptr(q_weight, torch.bfloat16, dim)
-    pkw = _dptr(k_weight, torch.bfloat16, dim)
-    if rope is not None and positions is None:
-        raise ValueError("a rotation needs positions")
-    pp = _dptr(positions, torch.int32, tokens)
-    _check("eq_qk_norm_rope",
-           lib().eq_qk_norm_rope(pq, sq, heads, pqw, pqo, pk, sk, hk, pkw, pko, kind, tokens, dim,
-                                 eps, pp, None if rope is None else rope.ptr, _stream(stream)))
+        shape = k.shape
+        n, hk, kd = shape
+        pk, sk, kind_k = _head_rows(k, shape, "k")
+        if n != tokens or kd != dim or kind_k != kind:
+            raise ValueError("q and k differ in tokens, head_dim or type")
+        pko = _bf16(k_out, tokens * hk * dim, "k_out")
+    pr = None
+    if rope is not None:
+        if positions is None:
+            raise ValueError("a rotation needs positions")
+        pr = rope.ptr
+    rc = lib().eq_qk_norm_rope(pq, sq, heads, _bf16(q_weight, dim, "q_weight"), pqo, pk, sk, hk,
+                               _bf16(k_weight, dim, "k_weight"), pko, kind, tokens, dim, eps,
+                               _positions(positions, tokens), pr, _stream(stream))
+    if rc:
+        raise EqError("eq_qk_norm_rope", rc)
 
 
 def eq_kv_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
@@ -509,25 +540,25 @@ def eq_kv_append(cache, batch, k, v, *, rope=None, positions=None, stream=None) 
     """Append k and v [n_tokens, kv_heads, head_dim] (fp32 or BF16), the keys
     rotated on the way when rope is given: at `positions`, or at the tokens'
     places in their sequences."""
-    import torch
-    pk, sk, kind = _head_rows(k, cache.kv_heads, cache.head_dim, "k")
-    pv, sv, kind_v = _head_rows(v, cache.kv_heads, cache.head_dim, "v")
+    pk, sk, kind = _cache_rows(k, cache, batch, "k")
+    pv, sv, kind_v = _cache_rows(v, cache, batch, "v")
     if kind != kind_v:
         raise ValueError("k and v differ in type")
-    if k.shape[0] < batch.n_tokens or v.shape[0] < batch.n_tokens:
-        raise ValueError("fewer rows than the batch's tokens")
-    pp = _dptr(positions, torch.int32, batch.n_tokens)
-    _check("eq_kv_append",
-           lib().eq_kv_append(cache.ptr, batch.ptr, pk, sk, pv, sv, kind, pp,
-                              None if rope is None else rope.ptr, _stream(stream)))
+    rc = lib().eq_kv_append(cache.ptr, batch.ptr, pk, sk, pv, sv, kind,
+                            _positions(positions, batch.n_tokens),
+                            None if rope is None else rope.ptr, _stream(stream))
+    if rc:
+        raise EqError("eq_kv_append", rc)
 
 
 def eq_kv_read(cache, batch, k, v, stream=None) -> None:
     """The cache's values of the batch's tokens, as BF16: k and v contiguous
     [n_tokens, kv_heads, head_dim]."""
     n = batch.n_tokens * cache.kv_heads * cache.head_dim
-    _check("eq_kv_read", lib().eq_kv_read(cache.ptr, batch.ptr, _bf16_out(k, n, "k"),
-                                          _bf16_out(v, n, "v"), _stream(stream)))
+    rc = lib().eq_kv_read(cache.ptr, batch.ptr, _bf16(k, n, "k"), _bf16(v, n, "v"),
+                          _stream(stream))
+    if rc:
+        raise EqError("eq_kv_read", rc)
 
 
 def eq_attn_kv4_workspace_bytes(cache, batch, q_heads: int) -> int:
@@ -546,16 +577,18 @@ def eq_attn_kv4(cache, batch, q, scale: float, out, ws=None, *, window: int = 0,
     """Causal attention of q [n_tokens, q_heads, head_dim] (BF16) over the
     cache to out (BF16, contiguous); with window, over the last `window`
     positions only."""
-    heads = q.shape[1]
-    pq, sq, kind = _head_rows(q, heads, cache.head_dim, "q")
-    if kind != 1:
-        raise ValueError("q: expected bfloat16")
-    if q.shape[0] < batch.n_tokens:
-        raise ValueError("fewer rows than the batch's tokens")
-    po = _bf16_out(out, batch.n_tokens * heads * cache.head_dim, "out")
+    shape = q.shape
+    n, heads, dim = shape
+    pq, sq, kind = _head_rows(q, shape, "q")
+    if kind != 1 or dim != cache.head_dim or n < batch.n_tokens:
+        raise ValueError(f"q: expected bfloat16 [{batch.n_tokens} tokens, heads, "
+                         f"{cache.head_dim}]")
+    po = _bf16(out, batch.n_tokens * heads * dim, "out")
     pw, nbytes = (None, 0) if ws is None else (_dptr(ws), ws.numel() * ws.element_size())
-    _check("eq_attn_kv4", lib().eq_attn_kv4(cache.ptr, batch.ptr, pq, sq, heads, scale, window, po,
-                                            pw, nbytes, _stream(stream)))
+    rc = lib().eq_attn_kv4(cache.ptr, batch.ptr, pq, sq, heads, scale, window, po, pw, nbytes,
+                           _stream(stream))
+    if rc:
+        raise EqError("eq_attn_kv4", rc)
 
 
 # ---------------------------------------------------------------- encoder ABI
