@@ -30,8 +30,12 @@ typedef short short2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t kTile = 128;  // tokens a wavefront takes at a time
-constexpr uint32_t kCols = 16;   // query columns of a block
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// Few query columns (attn_kernel): tokens a wavefront takes at a time, and the
+// columns of a block.  Many (prompt_kernel): tokens and columns of a block.
+constexpr uint32_t kTile = 128, kCols = 16;
+constexpr uint32_t kPromptTile = 64, kPromptCols = 128;
 constexpr uint32_t kWaves = 4;
 constexpr int kUnitScale = 127;  // scale byte of 1
 
@@ -40,7 +44,7 @@ struct AttnArgs {
   const uint16_t *q;
   uint64_t q_stride;
   uint16_t *out;
-  float *part;       // [n_seqs][kv_heads][q_tiles][chunks][kCols][D] sums of a chunk
+  float *part;       // [n_seqs][kv_heads][q_tiles][chunks][columns][D] sums of a chunk
   float2 *stat;      // the same without D: maximum and sum of P
   uint32_t group;    // query heads of a key/value head
   uint32_t window;
@@ -48,11 +52,12 @@ struct AttnArgs {
   float c;           // scale log2 e
 };
 
-// Columns [col0, col0 + kCols) of a sequence, and the cached tokens they see.
+// Columns [col0, col0 + COLS) of a sequence, and the cached tokens they see.
 struct Span {
   uint32_t cols;          // columns of the sequence
-  uint32_t first, last;   // token tiles [first, last)
+  uint32_t first, last;   // tiles [first, last) of TILE tokens
   uint32_t chunks;
+  uint32_t seen;          // tokens [0, seen) hold all that is seen
   int32_t hi_min, lo_max; // tokens in [lo_max, hi_min) are seen by every column
 };
 
@@ -61,17 +66,18 @@ __device__ inline int32_t start_of(uint32_t window, int32_t pos) {
   return window && pos >= 0 && uint32_t(pos) >= window ? pos + 1 - int32_t(window) : 0;
 }
 
+template <uint32_t COLS, uint32_t TILE>
 __device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
   Span p{};
   p.cols = uint32_t(q.count) * a.group;
   if (col0 >= p.cols) return p;
   const int32_t pos0 = q.base + int32_t(col0 / a.group);
-  const int32_t pos1 = q.base + int32_t((min(col0 + kCols, p.cols) - 1) / a.group);
+  const int32_t pos1 = q.base + int32_t((min(col0 + COLS, p.cols) - 1) / a.group);
   p.hi_min = end_of(q, pos0);
   p.lo_max = start_of(a.window, pos1);
-  const uint32_t lo = uint32_t(start_of(a.window, pos0)), hi = uint32_t(end_of(q, pos1));
-  p.first = lo / kTile;
-  p.last = max((hi + kTile - 1) / kTile, p.first);
+  p.seen = uint32_t(end_of(q, pos1));
+  p.first = uint32_t(start_of(a.window, pos0)) / TILE;
+  p.last = max((p.seen + TILE - 1) / TILE, p.first);
   p.chunks = (p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles;
   return p;
 }
@@ -157,6 +163,12 @@ struct Query {
 
 __device__ inline int8v widen(int4v v) { return int8v{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
 
+// acc + codes x terms: 32 x 32 over 64 steps, the codes' scales in byte BYTE of as.
+template <int BYTE>
+__device__ inline floatx16 mul32(int8v codes, int8v terms, floatx16 acc, int as, int bs) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes, terms, acc, 4, 0, BYTE, as, 0, bs);
+}
+
 // One block: kCols query columns of a key/value head against a chunk of token
 // tiles, dealt to its 4 wavefronts in turn; each keeps its own maximum, sum and
 // O, joined through LDS at the end.
@@ -180,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const uint32_t qt = rest % a.q_tiles, h = rest / a.q_tiles;
   const Seq q = sequence(w, s);
   const uint32_t col0 = qt * kCols;
-  const Span sp = span_of(a, q, col0);
+  const Span sp = span_of<kCols, kTile>(a, q, col0);
   if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t col = lane & 15, g = lane >> 4;
@@ -202,8 +214,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
 
   // addresses: the four 32-token units of a tile may be in four pages
   const int32_t *const table = w.page_table + size_t(s) * w.max_pages;
-  const uint32_t seen = uint32_t(end_of(q, q.base + int32_t((min(col0 + kCols, sp.cols) - 1) / a.group)));
-  const uint32_t last_unit = seen ? (seen - 1) / kUnit : 0;
+  const uint32_t last_unit = sp.seen ? (sp.seen - 1) / kUnit : 0;
   const uint32_t page_mask = (1u << w.page_shift) - 1;
   const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
   auto first_token = [&](uint32_t tile, uint32_t unit) {
@@ -416,9 +427,310 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   for (uint32_t i = 0; i < kPer; ++i) a.part[slot * D + d0 + i] = sum[i];
 }
 
+// The query columns of a wavefront of prompt_kernel: lane (col of 32, half) of
+// the operand of 64 steps holds steps 16 half .. + 15 and 32 + 16 half .. + 15,
+// and the scale of steps 32 half ..  One operand for 64 channels.
+template <int D>
+struct PromptQuery {
+  int8v h[D / 64], l[D / 64];
+  int hs[D / 64], ls[D / 64];
+  __device__ inline void load(const uint16_t *row, uint32_t half) {
+#pragma unroll
+    for (int kk = 0; kk < D / 64; ++kk) {
+      int byte[2];
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        uint32_t u[8] = {};
+        if (row) {
+          const uint4 *const p =
+              reinterpret_cast<const uint4 *>(row + 64 * kk + 32 * part + 16 * half);
+          *reinterpret_cast<uint4 *>(u) = p[0];
+          *reinterpret_cast<uint4 *>(u + 4) = p[1];
+        }
+        uint32_t top = 0;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[2 * i] = __uint_as_float(u[i] << 16);
+          x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+          top = max(top, max(u[i] << 16 & 0x7FFFFFFFu, u[i] & 0x7FFF0000u));
+        }
+        byte[part] = top_byte(max(top, uint32_t(__shfl_xor(int(top), 32))));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          int a, b;
+          split4(x + 4 * i, byte_value(byte[part]), a, b);
+          h[kk][4 * part + i] = a;
+          l[kk][4 * part + i] = b;
+        }
+      }
+      hs[kk] = half ? byte[1] : byte[0];
+      ls[kk] = low_byte(hs[kk]);
+    }
+  }
+};
+
+// Many query columns: a block of 4 wavefronts with 32 columns each, that share
+// tiles of 64 tokens through LDS (as codes; two buffers, the next tile's loads
+// in flight while one is multiplied).
+//
+// The layout is attn_kernel's with products of 32 x 32: lane (col, half) gets
+// rows 8 a + 4 half + e of its column and has to hold steps 16 half .. + 15 of
+// the lower and of the upper 32 tokens, so that row 8 a + 4 b + e of product T is
+// token 32 T + 16 b + 4 a + e.
+//
+// The running maximum follows the scores only when they pass it by more than
+// 8 (P then stays below 2^8): O is rescaled a few times in all, not whenever one
+// of 32 columns finds a larger score.
+template <int D>
+__global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
+  constexpr int ND = D / 32, KK = D / 64;
+  constexpr uint32_t kRow = D / 2 + 16;  // bytes a key in LDS: 16 rows start in 16 banks
+  constexpr uint32_t kV = kPromptTile * kRow, kKS = kV + kPromptTile * D / 2, kW = kKS + 256,
+                     kGone = kW + kPromptTile * 4, kBuf = kGone + 16;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
+  const View &w = a.w;
+  const uint32_t s = blockIdx.y;
+  // heads first (the blocks of a head on one XCD, whose L2 then holds its
+  // cache), and a sequence's last queries, which see most, before its first
+  const uint32_t h = blockIdx.x % w.kv_heads, rest = blockIdx.x / w.kv_heads;
+  const uint32_t chunk = rest % a.chunks, qt = a.q_tiles - 1 - rest / a.chunks;
+  const Seq q = sequence(w, s);
+  const uint32_t col0 = qt * kPromptCols;
+  const Span sp = span_of<kPromptCols, kPromptTile>(a, q, col0);
+  if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t col = lane & 31, half = lane >> 5;
+
+  const uint32_t wave_col = col0 + wave * 32, index = wave_col + col;
+  const bool real = index < sp.cols;
+  const uint32_t token = index / a.group;
+  const int32_t pos = q.base + int32_t(token);
+  const int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
+  const uint16_t *const row =
+      real ? a.q + uint64_t(q.row + token) * a.q_stride + uint64_t(h * a.group + index % a.group) * D
+           : nullptr;
+  PromptQuery<D> query;
+  query.load(row, half);
+  // the wavefront's own span: tokens that some column, and that every one sees
+  int32_t w_lo = 0, w_hi = 0, all_lo = 0, all_hi = 0;
+  if (wave_col < sp.cols) {
+    const int32_t p0 = q.base + int32_t(wave_col / a.group);
+    const int32_t p1 = q.base + int32_t((min(wave_col + 32, sp.cols) - 1) / a.group);
+    w_lo = start_of(a.window, p0), w_hi = end_of(q, p1);
+    all_lo = start_of(a.window, p1), all_hi = end_of(q, p0);
+  }
+
+  // staging: a thread's 16 bytes of key codes and of value codes, a key scale
+  // byte, and the first 64 threads a value scale each
+  const int32_t *const table = w.page_table + size_t(s) * w.max_pages;
+  const uint32_t last_unit = sp.seen ? (sp.seen - 1) / kUnit : 0;
+  const uint32_t page_mask = (1u << w.page_shift) - 1;
+  const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
+  // (D threads copy a unit: D x 16 bytes of key codes, as many of value codes
+  // and D key scales)
+  const uint32_t unit = tid / D, piece = tid % D;
+  const bool copies = unit < 2;
+  auto unit_of = [&](uint32_t tile, uint32_t u) { return min(2 * tile + u, last_unit) * kUnit; };
+  auto load_id = [&](uint32_t tile, uint32_t u) {
+    return table[unit_of(tile, u) >> w.page_shift];
+  };
+  auto part_of = [&](int id) {
+    return base + (uint32_t(id) < w.n_pages ? uint64_t(uint32_t(id)) : 0) * w.page_bytes;
+  };
+  struct Stage {
+    uint4 k, v;
+    uint32_t ks, vs;  // vs: a value scale byte, 256 for a token that is not there
+    bool gone;
+  };
+  auto load_tile = [&](uint32_t tile, int id, int id_w) {
+    Stage x{};
+    if (copies) {
+      const uint32_t slot = unit_of(tile, unit) & page_mask;
+      const uint8_t *const p = part_of(id);
+      x.k = *reinterpret_cast<const uint4 *>(p + slot * (D / 2) + piece * 16);
+      x.v = *reinterpret_cast<const uint4 *>(p + w.v_off + slot * (D / 2) + piece * 16);
+      x.ks = p[w.ks_off + slot * (D / 32) + piece];
+    }
+    if (tid < kPromptTile) {
+      const uint32_t slot = unit_of(tile, tid / kUnit) & page_mask;
+      x.gone = uint32_t(id_w) >= w.n_pages;
+      x.vs = part_of(id_w)[w.vs_off + slot + tid % kUnit];
+      if (x.gone || tile * kPromptTile + tid >= sp.seen) x.vs = 256;
+    }
+    return x;
+  };
+  const uint32_t k_to = (unit * kUnit + piece / (D / 32)) * kRow + piece % (D / 32) * 16;
+  const uint32_t ks_row = 8 * (piece % 4) + 4 * (piece / (D / 2)) + piece % (D / 2) / (D / 8);
+  const uint32_t ks_blk = piece / 4 % (D / 32);
+  const uint32_t ks_to = kKS + ((ks_blk & 1) * 32 + ks_row) * 4 + unit * 2 + (ks_blk >> 1);
+  auto store_tile = [&](uint8_t *buf, const Stage &x) {
+    if (copies) {
+      *reinterpret_cast<uint4 *>(buf + k_to) = x.k;
+      *reinterpret_cast<uint4 *>(buf + kV + tid * 16) = x.v;
+      buf[ks_to] = uint8_t(x.ks);
+    }
+    if (tid < kPromptTile) {
+      *reinterpret_cast<float *>(buf + kW + 4 * tid) = __uint_as_float((x.vs & 255u) << 23);
+      if (tid % kUnit == 0) *reinterpret_cast<uint32_t *>(buf + kGone + tid / kUnit * 4) = x.gone;
+    }
+  };
+
+  float m_run = -INFINITY, m_use = 0.0f, l_run = 0.0f;
+  floatx16 o[ND];
+#pragma unroll
+  for (int m = 0; m < ND; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[m][i] = 0.0f;
+  // this lane's row of a key product: row 8 a + 4 b + e is token 16 b + 4 a + e
+  const uint32_t krow = (col >> 2 & 1) * 16 + (col >> 3) * 4 + (col & 3);
+
+  auto compute = [&](uint32_t tile, const uint8_t *buf) {
+    const int32_t at = int32_t(tile * kPromptTile);
+    if (at >= w_hi || at + int32_t(kPromptTile) <= w_lo) return;
+    floatx16 sc[2];
+    const int ks = *reinterpret_cast<const int *>(buf + kKS + lane * 4);
+    auto keys = [&](int t, int kk) {
+      return widen(*reinterpret_cast<const int4v *>(buf + (t * kUnit + krow) * kRow + 32 * kk +
+                                                    16 * half));
+    };
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+    {
+      const int8v k0 = keys(0, 0), k1 = keys(1, 0);
+      sc[0] = mul32<0>(k0, query.h[0], sc[0], ks, query.hs[0]);
+      sc[1] = mul32<2>(k1, query.h[0], sc[1], ks, query.hs[0]);
+      sc[0] = mul32<0>(k0, query.l[0], sc[0], ks, query.ls[0]);
+      sc[1] = mul32<2>(k1, query.l[0], sc[1], ks, query.ls[0]);
+    }
+    if constexpr (KK == 2) {
+      const int8v k0 = keys(0, 1), k1 = keys(1, 1);
+      sc[0] = mul32<1>(k0, query.h[1], sc[0], ks, query.hs[1]);
+      sc[1] = mul32<3>(k1, query.h[1], sc[1], ks, query.hs[1]);
+      sc[0] = mul32<1>(k0, query.l[1], sc[0], ks, query.ls[1]);
+      sc[1] = mul32<3>(k1, query.l[1], sc[1], ks, query.ls[1]);
+    }
+    const uint32_t gone0 = *reinterpret_cast<const uint32_t *>(buf + kGone);
+    const uint32_t gone1 = *reinterpret_cast<const uint32_t *>(buf + kGone + 4);
+    uint32_t visible = ~0u;  // bit 16 t + i: this lane's column sees that token
+    if (at + int32_t(kPromptTile) > all_hi || at < all_lo || eq_dev::uniform(gone0 | gone1)) {
+      visible = 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int32_t tok = at + 32 * t + 16 * int32_t(half) + i;
+          const bool ok = tok >= lo && tok < hi && !(t ? gone1 : gone0);
+          visible |= uint32_t(ok) << (16 * t + i);
+          if (!ok) sc[t][i] = -INFINITY;
+        }
+    }
+    float mx = sc[0][0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[t][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.c;
+    if (__any(mx > m_run + 8.0f)) {
+      const float m_new = mx > m_run + 8.0f ? mx : m_run;
+      m_use = m_new == -INFINITY ? 0.0f : m_new;
+      const float f = exp2_(m_run - m_use);
+      m_run = m_new;
+      l_run *= f;
+#pragma unroll
+      for (int m = 0; m < ND; ++m) o[m] *= f;
+    }
+    float y[32], top = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const floatx4 wt = *reinterpret_cast<const floatx4 *>(buf + kW + (32 * t + 16 * half + i) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = exp2_(__builtin_fmaf(sc[t][i + e], a.c, -m_use));
+          l_run += p;
+          y[16 * t + i + e] = p * wt[e];
+        }
+      }
+    if (visible != ~0u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (!(visible >> i & 1)) y[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const int ps = top_byte(__float_as_uint(top)), pl = low_byte(ps);
+    const float scale = byte_value(ps);
+    int8v ph, pq;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      int u, v;
+      split4(y + 4 * i, scale, u, v);
+      ph[i] = u;
+      pq[i] = v;
+    }
+#pragma unroll
+    for (int m = 0; m < ND; ++m) {
+      const int8v v8 =
+          widen(*reinterpret_cast<const int4v *>(buf + kV + (half * D + 32 * m + col) * 16));
+      o[m] = mul32<0>(v8, ph, o[m], kUnitScale, ps);
+      o[m] = mul32<0>(v8, pq, o[m], kUnitScale, pl);
+    }
+  };
+
+  const uint32_t t0 = sp.first + chunk * a.chunk_tiles, t1 = min(t0 + a.chunk_tiles, sp.last);
+  if (t0 < t1) {
+    const uint32_t id_unit = copies ? unit : 0, w_unit = tid / kUnit & 1;
+    int id = load_id(t0, id_unit), id_w = load_id(t0, w_unit);
+    store_tile(lds, load_tile(t0, id, id_w));
+    id = load_id(t0 + 1, id_unit), id_w = load_id(t0 + 1, w_unit);
+    __syncthreads();
+    for (uint32_t t = t0; t < t1; ++t) {
+      Stage x{};
+      const bool more = t + 1 < t1;
+      if (more) {
+        x = load_tile(t + 1, id, id_w);
+        id = load_id(t + 2, id_unit), id_w = load_id(t + 2, w_unit);
+      }
+      compute(t, lds + (t - t0 & 1) * kBuf);
+      if (more) store_tile(lds + (t + 1 - t0 & 1) * kBuf, x);
+      __syncthreads();
+    }
+  }
+  l_run += __shfl_xor(l_run, 32);
+  if (!real) return;
+  if (sp.chunks <= 1) {
+    const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+    uint16_t *const out = a.out + (uint64_t(q.row + token) * w.kv_heads * a.group + h * a.group +
+                                   index % a.group) * D + 4 * half;
+#pragma unroll
+    for (int m = 0; m < ND; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<uint2 *>(out + 32 * m + 2 * i) =
+            make_uint2(eq_dev::pack_bf16(o[m][i] * inv, o[m][i + 1] * inv),
+                       eq_dev::pack_bf16(o[m][i + 2] * inv, o[m][i + 3] * inv));
+    return;
+  }
+  const uint64_t slot =
+      (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks + chunk) * kPromptCols +
+      wave * 32 + col;
+  if (half == 0) a.stat[slot] = make_float2(m_run, l_run);
+#pragma unroll
+  for (int m = 0; m < ND; ++m)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<floatx4 *>(a.part + slot * D + 32 * m + 2 * i + 4 * half) =
+          floatx4{o[m][i], o[m][i + 1], o[m][i + 2], o[m][i + 3]};
+}
+
 // Joins the chunks of one query head at one new token, a block each: 8
 // sub-blocks of threads take the chunks in turn, then add up through LDS.
-template <int D>
+template <int D, uint32_t COLS, uint32_t TILE>
 __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   constexpr uint32_t kLanes = D / 4, kSub = 8;
   __shared__ __attribute__((aligned(16))) float4 lds[kSub][kLanes];
@@ -429,19 +741,20 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   const Seq q = sequence(w, s);
   if (int32_t(token) >= q.count) return;
   const uint32_t h = head / a.group, index = token * a.group + head % a.group;
-  const uint32_t qt = index / kCols;
-  const Span sp = span_of(a, q, qt * kCols);
+  const uint32_t qt = index / COLS;
+  const Span sp = span_of<COLS, TILE>(a, q, qt * COLS);
   if (sp.chunks <= 1) return;
-  const uint64_t first = (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * kCols + index % kCols;
+  const uint64_t first =
+      (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * COLS + index % COLS;
   float m = -INFINITY;
-  for (uint32_t c = 0; c < sp.chunks; ++c) m = fmaxf(m, a.stat[first + uint64_t(c) * kCols].x);
+  for (uint32_t c = 0; c < sp.chunks; ++c) m = fmaxf(m, a.stat[first + uint64_t(c) * COLS].x);
   if (m == -INFINITY) m = 0.0f;
   const uint32_t sub = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
   float4 o = make_float4(0, 0, 0, 0);
   float total = 0.0f;
 #pragma unroll 4
   for (uint32_t c = sub; c < sp.chunks; c += kSub) {
-    const uint64_t at = first + uint64_t(c) * kCols;
+    const uint64_t at = first + uint64_t(c) * COLS;
     const float2 st = a.stat[at];
     const float4 x = *reinterpret_cast<const float4 *>(a.part + at * D + 4 * l);
     const float f = exp2_(st.x - m);
@@ -463,33 +776,61 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
       make_uint2(eq_dev::pack_bf16(o.x * inv, o.y * inv), eq_dev::pack_bf16(o.z * inv, o.w * inv));
 }
 
-// How a call is launched: chunks of token tiles so that the blocks fill the
-// card about twice over, none shorter than a tile for each wavefront, and up to
-// 2048 query tiles none longer than 32 tiles (a ragged batch's longest sequence
-// then spreads over the card too).
+// How a call is launched.  Up to kFewCols columns of a key/value head and
+// sequence go to attn_kernel, more to prompt_kernel.  The token tiles are cut
+// into chunks so that the blocks fill the card about twice over, none shorter
+// than four tiles (attn_kernel: one for each wavefront) and, where there is less
+// than that to fill it with, none longer than 4096 tokens: a ragged batch's
+// longest sequence then spreads over the card too.
 struct Plan {
-  uint32_t q_tiles, chunks, chunk_tiles;
+  bool prompt;
+  uint32_t cols, tile, q_tiles, chunks, chunk_tiles;
 };
+
+constexpr uint32_t kFewCols = 64;
 
 Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_new,
                uint32_t max_len) {
   Plan p;
-  p.q_tiles = uint32_t((uint64_t(max_new) * group + kCols - 1) / kCols);
+  const uint64_t cols = uint64_t(max_new) * group;
+  p.prompt = cols > kFewCols;
+  p.cols = p.prompt ? kPromptCols : kCols;
+  p.tile = p.prompt ? kPromptTile : kTile;
+  p.q_tiles = uint32_t((cols + p.cols - 1) / p.cols);
   const uint64_t work = uint64_t(n_seqs) * kv_heads * p.q_tiles;
-  const uint32_t tiles = (max_len + kTile - 1) / kTile;
+  const uint32_t tiles = (max_len + p.tile - 1) / p.tile;
   const uint64_t want = std::max<uint64_t>(1, (512 + work - 1) / work);
   uint32_t ct = uint32_t((tiles + want - 1) / want);
-  ct = std::max((ct + kWaves - 1) / kWaves * kWaves, kWaves);
-  if (work <= 2048) ct = std::min(ct, 32u);
+  ct = std::max((ct + 3) / 4 * 4, 4u);
+  if (work < (p.prompt ? 512 : 2048)) ct = std::min(ct, 4096 / p.tile);
   p.chunk_tiles = ct;
   p.chunks = std::max((tiles + ct - 1) / ct, 1u);
   return p;
 }
 
+// Columns of partial results: a sum for each channel, a maximum and a sum of P.
+size_t part_cols(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
+  return size_t(b->n_seqs) * c->kv_heads * p.q_tiles * p.chunks * p.cols;
+}
+
 size_t attn_bytes(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
-  if (p.chunks <= 1) return 0;
-  return size_t(b->n_seqs) * c->kv_heads * p.q_tiles * p.chunks * kCols * (c->head_dim + 2) *
-         sizeof(float);
+  return p.chunks <= 1 ? 0 : part_cols(p, c, b) * (c->head_dim + 2) * sizeof(float);
+}
+
+template <int D>
+void launch_attn(const AttnArgs &a, const Plan &p, bool one_page, dim3 grid, dim3 join,
+                 hipStream_t stream) {
+  const dim3 block(256), join_block(2 * D);
+  if (p.prompt) {
+    hipLaunchKernelGGL(prompt_kernel<D>, grid, block, 0, stream, a);
+    if (p.chunks > 1)
+      hipLaunchKernelGGL((join_kernel<D, kPromptCols, kPromptTile>), join, join_block, 0, stream, a);
+    return;
+  }
+  if (one_page) hipLaunchKernelGGL((attn_kernel<D, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((attn_kernel<D, false>), grid, block, 0, stream, a);
+  if (p.chunks > 1)
+    hipLaunchKernelGGL((join_kernel<D, kCols, kTile>), join, join_block, 0, stream, a);
 }
 
 bool heads_ok(const eq_kv_cache *c, uint32_t q_heads) {
@@ -527,17 +868,10 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
   AttnArgs a{view(cache, batch), q, q_stride, out, static_cast<float *>(ws), nullptr, group, window,
              p.q_tiles, p.chunks, p.chunk_tiles, scale * 1.44269504088896340736f};
   if (need)
-    a.stat = reinterpret_cast<float2 *>(a.part + size_t(batch->n_seqs) * cache->kv_heads * p.q_tiles *
-                                                     p.chunks * kCols * cache->head_dim);
+    a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
   const dim3 grid(uint32_t(blocks), batch->n_seqs), join(uint32_t(joins), batch->n_seqs);
-  const bool one = cache->page_tokens >= kTile;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
-  if (cache->head_dim == 128) {
-    one ? go(attn_kernel<128, true>) : go(attn_kernel<128, false>);
-    if (p.chunks > 1) hipLaunchKernelGGL(join_kernel<128>, join, dim3(256), 0, stream, a);
-  } else {
-    one ? go(attn_kernel<64, true>) : go(attn_kernel<64, false>);
-    if (p.chunks > 1) hipLaunchKernelGGL(join_kernel<64>, join, dim3(128), 0, stream, a);
-  }
+  const bool one_page = cache->page_tokens >= kTile;
+  if (cache->head_dim == 128) launch_attn<128>(a, p, one_page, grid, join, stream);
+  else launch_attn<64>(a, p, one_page, grid, join, stream);
   return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP;
 }
