@@ -84,7 +84,9 @@ __device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
 
 // x / scale as two E4M3 terms, of four values: h at `scale`, l at scale / 16.
 __device__ inline void split4(const float *x, float scale, int &h, int &l) {
-  short2v a = {0, 0}, b = {0, 0};
+  short2v a, b;  // each conversion fills one half
+  a = __builtin_nondeterministic_value(a);
+  b = __builtin_nondeterministic_value(b);
   a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, x[0], x[1], scale, false);
   a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, x[2], x[3], scale, true);
   h = __builtin_bit_cast(int, a);
@@ -194,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const uint32_t col0 = qt * kCols;
   const Span sp = span_of<kCols, kTile>(a, q, col0);
   if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
   const uint32_t col = lane & 15, g = lane >> 4;
 
   // this lane's column
@@ -314,9 +316,9 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     }
     // masks, only where some column does not see the whole tile
     const int32_t at = int32_t(t * kTile);
-    uint32_t visible = ~0u;  // bit 4 i + r: this lane's column sees that token
-    if (at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || __any(bad_a || bad_b)) {
-      visible = 0;
+    uint32_t visible = 0;  // bit 4 i + r: this lane's column sees that token
+    const bool masked = at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || __any(bad_a || bad_b);
+    if (masked) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
         l_run += p;
         y[4 * i + e] = p * __uint_as_float((vs[i] >> (8 * e) & 255u) << 23);
       }
-    if (visible != ~0u) {
+    if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
 #pragma unroll
       for (int i = 0; i < 32; ++i)
         if (!(visible >> i & 1)) y[i] = 0.0f;
@@ -499,7 +501,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   const uint32_t col0 = qt * kPromptCols;
   const Span sp = span_of<kPromptCols, kPromptTile>(a, q, col0);
   if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
-  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t tid = threadIdx.x, lane = tid & 63, wave = eq_dev::uniform(tid >> 6);
   const uint32_t col = lane & 31, half = lane >> 5;
 
   const uint32_t wave_col = col0 + wave * 32, index = wave_col + col;
@@ -521,42 +523,34 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
     all_lo = start_of(a.window, p1), all_hi = end_of(q, p0);
   }
 
-  // staging: a thread's 16 bytes of key codes and of value codes, a key scale
-  // byte, and the first 64 threads a value scale each
-  const int32_t *const table = w.page_table + size_t(s) * w.max_pages;
+  // staging: D threads copy a unit, 16 bytes of its key codes, 16 of its value
+  // codes and a key scale each (at D = 64 two wavefronts do), and the first 32
+  // of them a value scale; what a wavefront copies is of one unit
+  const uint32_t *const table =
+      reinterpret_cast<const uint32_t *>(w.page_table + size_t(s) * w.max_pages);
   const uint32_t last_unit = sp.seen ? (sp.seen - 1) / kUnit : 0;
   const uint32_t page_mask = (1u << w.page_shift) - 1;
   const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
-  // (D threads copy a unit: D x 16 bytes of key codes, as many of value codes
-  // and D key scales)
-  const uint32_t unit = tid / D, piece = tid % D;
-  const bool copies = unit < 2;
-  auto unit_of = [&](uint32_t tile, uint32_t u) { return min(2 * tile + u, last_unit) * kUnit; };
-  auto load_id = [&](uint32_t tile, uint32_t u) {
-    return table[unit_of(tile, u) >> w.page_shift];
-  };
-  auto part_of = [&](int id) {
-    return base + (uint32_t(id) < w.n_pages ? uint64_t(uint32_t(id)) : 0) * w.page_bytes;
-  };
+  const uint32_t unit = wave * 64 / D, piece = tid % D;
+  const bool copies = unit < 2, scales = copies && wave * 64 % D == 0;
+  auto unit_of = [&](uint32_t tile) { return min(2 * tile + unit, last_unit) * kUnit; };
+  auto load_id = [&](uint32_t tile) { return eq_dev::as_const(table)[unit_of(tile) >> w.page_shift]; };
   struct Stage {
     uint4 k, v;
-    uint32_t ks, vs;  // vs: a value scale byte, 256 for a token that is not there
-    bool gone;
+    uint32_t ks, vs;
+    uint32_t id;
   };
-  auto load_tile = [&](uint32_t tile, int id, int id_w) {
+  auto load_tile = [&](uint32_t tile, uint32_t id) {
     Stage x{};
+    x.id = id;
     if (copies) {
-      const uint32_t slot = unit_of(tile, unit) & page_mask;
-      const uint8_t *const p = part_of(id);
-      x.k = *reinterpret_cast<const uint4 *>(p + slot * (D / 2) + piece * 16);
-      x.v = *reinterpret_cast<const uint4 *>(p + w.v_off + slot * (D / 2) + piece * 16);
-      x.ks = p[w.ks_off + slot * (D / 32) + piece];
-    }
-    if (tid < kPromptTile) {
-      const uint32_t slot = unit_of(tile, tid / kUnit) & page_mask;
-      x.gone = uint32_t(id_w) >= w.n_pages;
-      x.vs = part_of(id_w)[w.vs_off + slot + tid % kUnit];
-      if (x.gone || tile * kPromptTile + tid >= sp.seen) x.vs = 256;
+      const uint32_t slot = unit_of(tile) & page_mask;
+      const uint8_t *const p = base + uint64_t(id < w.n_pages ? id : 0) * w.page_bytes;
+      const uint32_t k_at = slot * (D / 2), lane16 = piece * 16;
+      x.k = *reinterpret_cast<const uint4 *>(p + k_at + lane16);
+      x.v = *reinterpret_cast<const uint4 *>(p + w.v_off + k_at + lane16);
+      x.ks = (p + w.ks_off + slot * (D / 32))[piece];
+      if (scales) x.vs = (p + w.vs_off + slot)[lane & 31];
     }
     return x;
   };
@@ -564,15 +558,20 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   const uint32_t ks_row = 8 * (piece % 4) + 4 * (piece / (D / 2)) + piece % (D / 2) / (D / 8);
   const uint32_t ks_blk = piece / 4 % (D / 32);
   const uint32_t ks_to = kKS + ((ks_blk & 1) * 32 + ks_row) * 4 + unit * 2 + (ks_blk >> 1);
-  auto store_tile = [&](uint8_t *buf, const Stage &x) {
-    if (copies) {
-      *reinterpret_cast<uint4 *>(buf + k_to) = x.k;
-      *reinterpret_cast<uint4 *>(buf + kV + tid * 16) = x.v;
-      buf[ks_to] = uint8_t(x.ks);
-    }
-    if (tid < kPromptTile) {
-      *reinterpret_cast<float *>(buf + kW + 4 * tid) = __uint_as_float((x.vs & 255u) << 23);
-      if (tid % kUnit == 0) *reinterpret_cast<uint32_t *>(buf + kGone + tid / kUnit * 4) = x.gone;
+  auto store_tile = [&](uint8_t *buf, uint32_t tile, const Stage &x) {
+    if (!copies) return;
+    *reinterpret_cast<uint4 *>(buf + k_to) = x.k;
+    *reinterpret_cast<uint4 *>(buf + kV + tid * 16) = x.v;
+    buf[ks_to] = uint8_t(x.ks);
+    if (scales) {
+      // scales of tokens behind the last one seen, or of a page that is not
+      // there, are anything: as 0
+      const bool gone = x.id >= w.n_pages;
+      const uint32_t left = sp.seen - min(tile * kPromptTile + unit * kUnit, sp.seen);
+      if (lane < kUnit)
+        *reinterpret_cast<float *>(buf + kW + 4 * (unit * kUnit + lane)) =
+            __uint_as_float(gone || lane >= left ? 0u : x.vs << 23);
+      if (lane == 0) *reinterpret_cast<uint32_t *>(buf + kGone + unit * 4) = gone;
     }
   };
 
@@ -614,9 +613,10 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
     }
     const uint32_t gone0 = *reinterpret_cast<const uint32_t *>(buf + kGone);
     const uint32_t gone1 = *reinterpret_cast<const uint32_t *>(buf + kGone + 4);
-    uint32_t visible = ~0u;  // bit 16 t + i: this lane's column sees that token
-    if (at + int32_t(kPromptTile) > all_hi || at < all_lo || eq_dev::uniform(gone0 | gone1)) {
-      visible = 0;
+    uint32_t visible = 0;  // bit 16 t + i: this lane's column sees that token
+    const bool masked = at + int32_t(kPromptTile) > all_hi || at < all_lo ||
+                        eq_dev::uniform(gone0 | gone1) != 0;
+    if (masked) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -648,14 +648,16 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
         const floatx4 wt = *reinterpret_cast<const floatx4 *>(buf + kW + (32 * t + 16 * half + i) * 4);
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = exp2_(__builtin_fmaf(sc[t][i + e], a.c, -m_use));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = exp2_(__builtin_fmaf(sc[t][i + e], a.c, -m_use));
-          l_run += p;
-          y[16 * t + i + e] = p * wt[e];
+          l_run += p[e];
+          y[16 * t + i + e] = p[e] * wt[e];
         }
       }
-    if (visible != ~0u) {
+    if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
 #pragma unroll
       for (int i = 0; i < 32; ++i)
         if (!(visible >> i & 1)) y[i] = 0.0f;
@@ -684,20 +686,19 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 
   const uint32_t t0 = sp.first + chunk * a.chunk_tiles, t1 = min(t0 + a.chunk_tiles, sp.last);
   if (t0 < t1) {
-    const uint32_t id_unit = copies ? unit : 0, w_unit = tid / kUnit & 1;
-    int id = load_id(t0, id_unit), id_w = load_id(t0, w_unit);
-    store_tile(lds, load_tile(t0, id, id_w));
-    id = load_id(t0 + 1, id_unit), id_w = load_id(t0 + 1, w_unit);
+    uint32_t id = load_id(t0);
+    store_tile(lds, t0, load_tile(t0, id));
+    id = load_id(t0 + 1);
     __syncthreads();
     for (uint32_t t = t0; t < t1; ++t) {
       Stage x{};
       const bool more = t + 1 < t1;
       if (more) {
-        x = load_tile(t + 1, id, id_w);
-        id = load_id(t + 2, id_unit), id_w = load_id(t + 2, w_unit);
+        x = load_tile(t + 1, id);
+        id = load_id(t + 2);
       }
-      compute(t, lds + (t - t0 & 1) * kBuf);
-      if (more) store_tile(lds + (t + 1 - t0 & 1) * kBuf, x);
+      compute(t, lds + ((t - t0) & 1) * kBuf);
+      if (more) store_tile(lds + ((t + 1 - t0) & 1) * kBuf, t + 1, x);
       __syncthreads();
     }
   }
