@@ -29,6 +29,7 @@ typedef int int8v __attribute__((ext_vector_type(8)));
 typedef short short2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
@@ -164,6 +165,12 @@ struct Query {
 };
 
 __device__ inline int8v widen(int4v v) { return int8v{v[0], v[1], v[2], v[3], 0, 0, 0, 0}; }
+
+// Codes 2 I and 2 I + 1 of a dword as BF16.
+template <int I>
+__device__ inline uint32_t code_pair(uint32_t codes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, 1.0f, I));
+}
 
 // acc + codes x terms: 32 x 32 over 64 steps, the codes' scales in byte BYTE of as.
 template <int BYTE>
@@ -476,20 +483,26 @@ struct PromptQuery {
 // tiles of 64 tokens through LDS (as codes; two buffers, the next tile's loads
 // in flight while one is multiplied).
 //
-// The layout is attn_kernel's with products of 32 x 32: lane (col, half) gets
-// rows 8 a + 4 half + e of its column and has to hold steps 16 half .. + 15 of
-// the lower and of the upper 32 tokens, so that row 8 a + 4 b + e of product T is
-// token 32 T + 16 b + 4 a + e.
+// Here the vector instructions of the softmax are the limit, and splitting w P
+// in two terms would be half of them.  So the second product takes w P as BF16
+// (8 significant bits as well, rounded to nearest), and the value codes are
+// brought to BF16 once for a block, when a tile is copied into LDS.
 //
-// The running maximum follows the scores only when they pass it by more than
-// 8 (P then stays below 2^8): O is rescaled a few times in all, not whenever one
-// of 32 columns finds a larger score.
+// The layout follows attn_kernel's idea: of a 32 x 32 product lane (col, half)
+// gets rows 8 a + 4 half + e of its column, and for 16 tokens of the second
+// product it has to hold tokens 8 half .. + 7; so row 16 b + 8 c + 4 d + e of a
+// unit's scores is its token 16 b + 8 d + 4 c + e.
+//
+// The maximum is set 8 above the scores, and follows when they reach it: P stays
+// at most 1, and O is rescaled a few times in all, not whenever one of 32 columns
+// finds a larger score.
 template <int D>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   constexpr int ND = D / 32, KK = D / 64;
   constexpr uint32_t kRow = D / 2 + 16;  // bytes a key in LDS: 16 rows start in 16 banks
-  constexpr uint32_t kV = kPromptTile * kRow, kKS = kV + kPromptTile * D / 2, kW = kKS + 256,
-                     kGone = kW + kPromptTile * 4, kBuf = kGone + 16;
+  constexpr uint32_t kVRow = kPromptTile * 2 + 16;  // bytes a channel's values, likewise
+  constexpr uint32_t kV = kPromptTile * kRow, kKS = kV + D * kVRow, kW = kKS + 256,
+                     kOdd = kW + kPromptTile * 4, kBuf = kOdd + 16;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
   const View &w = a.w;
   const uint32_t s = blockIdx.y;
@@ -555,23 +568,32 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
     return x;
   };
   const uint32_t k_to = (unit * kUnit + piece / (D / 32)) * kRow + piece % (D / 32) * 16;
-  const uint32_t ks_row = 8 * (piece % 4) + 4 * (piece / (D / 2)) + piece % (D / 2) / (D / 8);
+  const uint32_t ks_row = 16 * (piece / (D / 2)) + 8 * (piece & 1) + 4 * (piece >> 1 & 1) +
+                          piece % (D / 2) / (D / 8);
   const uint32_t ks_blk = piece / 4 % (D / 32);
   const uint32_t ks_to = kKS + ((ks_blk & 1) * 32 + ks_row) * 4 + unit * 2 + (ks_blk >> 1);
   auto store_tile = [&](uint8_t *buf, uint32_t tile, const Stage &x) {
     if (!copies) return;
     *reinterpret_cast<uint4 *>(buf + k_to) = x.k;
-    *reinterpret_cast<uint4 *>(buf + kV + tid * 16) = x.v;
+    const uint32_t codes[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint4 *>(buf + kV + piece * kVRow + unit * 64 + 16 * i) =
+          make_uint4(code_pair<0>(codes[i]), code_pair<1>(codes[i]), code_pair<2>(codes[i]),
+                     code_pair<3>(codes[i]));
     buf[ks_to] = uint8_t(x.ks);
     if (scales) {
-      // scales of tokens behind the last one seen, or of a page that is not
-      // there, are anything: as 0
+      // tokens behind the last one seen, or of a page that is not there, have
+      // any scale: 0; of those whose values are NaN there is a list, and theirs
+      // is 1 (a hidden token's P of 0 then stays 0)
       const bool gone = x.id >= w.n_pages;
       const uint32_t left = sp.seen - min(tile * kPromptTile + unit * kUnit, sp.seen);
+      const bool there = !gone && lane < min(left, kUnit);
+      const uint32_t nan = uint32_t(__ballot(there && x.vs == 255));
       if (lane < kUnit)
         *reinterpret_cast<float *>(buf + kW + 4 * (unit * kUnit + lane)) =
-            __uint_as_float(gone || lane >= left ? 0u : x.vs << 23);
-      if (lane == 0) *reinterpret_cast<uint32_t *>(buf + kGone + unit * 4) = gone;
+            there ? (x.vs == 255 ? 1.0f : __uint_as_float(x.vs << 23)) : 0.0f;
+      if (lane == 0) *reinterpret_cast<uint2 *>(buf + kOdd + unit * 8) = make_uint2(gone, nan);
     }
   };
 
@@ -581,22 +603,23 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   for (int m = 0; m < ND; ++m)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[m][i] = 0.0f;
-  // this lane's row of a key product: row 8 a + 4 b + e is token 16 b + 4 a + e
-  const uint32_t krow = (col >> 2 & 1) * 16 + (col >> 3) * 4 + (col & 3);
+  // this lane's key of a unit
+  const uint32_t krow = (col & 19) | (col >> 3 & 1) << 2 | (col >> 2 & 1) << 3;
+  const uint32_t k_from = krow * kRow + 16 * half, v_from = kV + col * kVRow + 16 * half;
 
   auto compute = [&](uint32_t tile, const uint8_t *buf) {
     const int32_t at = int32_t(tile * kPromptTile);
     if (at >= w_hi || at + int32_t(kPromptTile) <= w_lo) return;
+    const uint4 odd = *reinterpret_cast<const uint4 *>(buf + kOdd);  // gone, NaN of each unit
     floatx16 sc[2];
     const int ks = *reinterpret_cast<const int *>(buf + kKS + lane * 4);
-    auto keys = [&](int t, int kk) {
-      return widen(*reinterpret_cast<const int4v *>(buf + (t * kUnit + krow) * kRow + 32 * kk +
-                                                    16 * half));
+    auto keys = [&](int u, int kk) {
+      return widen(*reinterpret_cast<const int4v *>(buf + k_from + u * kUnit * kRow + 32 * kk));
     };
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) sc[u][i] = 0.0f;
     {
       const int8v k0 = keys(0, 0), k1 = keys(1, 0);
       sc[0] = mul32<0>(k0, query.h[0], sc[0], ks, query.hs[0]);
@@ -611,30 +634,29 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
       sc[0] = mul32<1>(k0, query.l[1], sc[0], ks, query.ls[1]);
       sc[1] = mul32<3>(k1, query.l[1], sc[1], ks, query.ls[1]);
     }
-    const uint32_t gone0 = *reinterpret_cast<const uint32_t *>(buf + kGone);
-    const uint32_t gone1 = *reinterpret_cast<const uint32_t *>(buf + kGone + 4);
-    uint32_t visible = 0;  // bit 16 t + i: this lane's column sees that token
-    const bool masked = at + int32_t(kPromptTile) > all_hi || at < all_lo ||
-                        eq_dev::uniform(gone0 | gone1) != 0;
-    if (masked) {
+    __builtin_amdgcn_s_setprio(1);  // ahead of the block's and the other block's products
+    // masks, where some column does not see some token
+    if (at + int32_t(kPromptTile) > all_hi || at < all_lo ||
+        eq_dev::uniform(odd.x | odd.y | odd.z | odd.w) != 0) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t gone = u ? odd.z : odd.x, nan = u ? odd.w : odd.y;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int32_t tok = at + 32 * t + 16 * int32_t(half) + i;
-          const bool ok = tok >= lo && tok < hi && !(t ? gone1 : gone0);
-          visible |= uint32_t(ok) << (16 * t + i);
-          if (!ok) sc[t][i] = -INFINITY;
+          const int32_t in = 16 * (i / 8) + 8 * int32_t(half) + i % 8, tok = at + 32 * u + in;
+          if (nan >> in & 1) sc[u][i] = NAN;
+          if (tok < lo || tok >= hi || gone) sc[u][i] = -INFINITY;
         }
+      }
     }
     float mx = sc[0][0];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[t][i]);
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
     mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.c;
-    if (__any(mx > m_run + 8.0f)) {
-      const float m_new = mx > m_run + 8.0f ? mx : m_run;
+    if (__any(mx > m_run)) {
+      const float m_new = mx > m_run ? mx + 8.0f : m_run;
       m_use = m_new == -INFINITY ? 0.0f : m_new;
       const float f = exp2_(m_run - m_use);
       m_run = m_new;
@@ -642,46 +664,32 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 #pragma unroll
       for (int m = 0; m < ND; ++m) o[m] *= f;
     }
-    float y[32], top = 0.0f;
+    uint4 p16[4];  // w P of 16 tokens each
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int g = 0; g < 4; ++g) {
+      uint32_t pk[4];
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const floatx4 wt = *reinterpret_cast<const floatx4 *>(buf + kW + (32 * t + 16 * half + i) * 4);
+      for (int j = 0; j < 8; j += 4) {
+        const floatx4 wt = *reinterpret_cast<const floatx4 *>(buf + kW + (16 * g + 8 * half + j) * 4);
         float p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = exp2_(__builtin_fmaf(sc[t][i + e], a.c, -m_use));
+        for (int e = 0; e < 4; ++e)
+          p[e] = exp2_(__builtin_fmaf(sc[g / 2][8 * (g & 1) + j + e], a.c, -m_use));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          l_run += p[e];
-          y[16 * t + i + e] = p[e] * wt[e];
-        }
+        for (int e = 0; e < 4; ++e) l_run += p[e];
+        pk[j / 2] = eq_dev::pack_bf16(p[0] * wt[0], p[1] * wt[1]);
+        pk[j / 2 + 1] = eq_dev::pack_bf16(p[2] * wt[2], p[3] * wt[3]);
       }
-    if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (!(visible >> i & 1)) y[i] = 0.0f;
+      p16[g] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
     }
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const int ps = top_byte(__float_as_uint(top)), pl = low_byte(ps);
-    const float scale = byte_value(ps);
-    int8v ph, pq;
+    for (int g = 0; g < 4; ++g)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      int u, v;
-      split4(y + 4 * i, scale, u, v);
-      ph[i] = u;
-      pq[i] = v;
-    }
-#pragma unroll
-    for (int m = 0; m < ND; ++m) {
-      const int8v v8 =
-          widen(*reinterpret_cast<const int4v *>(buf + kV + (half * D + 32 * m + col) * 16));
-      o[m] = mul32<0>(v8, ph, o[m], kUnitScale, ps);
-      o[m] = mul32<0>(v8, pq, o[m], kUnitScale, pl);
-    }
+      for (int m = 0; m < ND; ++m)
+        o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            *reinterpret_cast<const bf16x8 *>(buf + v_from + m * 32 * kVRow + 32 * g),
+            __builtin_bit_cast(bf16x8, p16[g]), o[m], 0, 0, 0);
   };
 
   const uint32_t t0 = sp.first + chunk * a.chunk_tiles, t1 = min(t0 + a.chunk_tiles, sp.last);
