@@ -480,8 +480,9 @@ struct PromptQuery {
 };
 
 // Many query columns: a block of 4 wavefronts with 32 columns each, that share
-// tiles of 64 tokens through LDS (as codes; two buffers, the next tile's loads
-// in flight while one is multiplied).
+// tiles of 64 tokens through LDS.  Three buffers: a tile's scores are multiplied
+// beside the softmax of the tile before, while the loads of the one after are in
+// flight.
 //
 // Here the vector instructions of the softmax are the limit, and splitting w P
 // in two terms would be half of them.  So the second product takes w P as BF16
@@ -503,7 +504,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   constexpr uint32_t kVRow = kPromptTile * 2 + 16;  // bytes a channel's values, likewise
   constexpr uint32_t kV = kPromptTile * kRow, kKS = kV + D * kVRow, kW = kKS + 256,
                      kOdd = kW + kPromptTile * 4, kBuf = kOdd + 16;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[3 * kBuf];
   const View &w = a.w;
   const uint32_t s = blockIdx.y;
   // heads first (the blocks of a head on one XCD, whose L2 then holds its
@@ -544,27 +545,26 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   const uint32_t last_unit = sp.seen ? (sp.seen - 1) / kUnit : 0;
   const uint32_t page_mask = (1u << w.page_shift) - 1;
   const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
-  const uint32_t unit = wave * 64 / D, piece = tid % D;
-  const bool copies = unit < 2, scales = copies && wave * 64 % D == 0;
+  const uint32_t unit = wave * 64 / D & 1, piece = tid % D;
+  const bool copies = wave * 64 / D < 2, scales = copies && wave * 64 % D == 0;
   auto unit_of = [&](uint32_t tile) { return min(2 * tile + unit, last_unit) * kUnit; };
   auto load_id = [&](uint32_t tile) { return eq_dev::as_const(table)[unit_of(tile) >> w.page_shift]; };
   struct Stage {
     uint4 k, v;
-    uint32_t ks, vs;
-    uint32_t id;
+    uint32_t ks, vs, id;
   };
+  // (Every thread loads, and past the last tile that one again: a load under a
+  // condition would be waited for where the branches meet.)
   auto load_tile = [&](uint32_t tile, uint32_t id) {
-    Stage x{};
+    Stage x;
     x.id = id;
-    if (copies) {
-      const uint32_t slot = unit_of(tile) & page_mask;
-      const uint8_t *const p = base + uint64_t(id < w.n_pages ? id : 0) * w.page_bytes;
-      const uint32_t k_at = slot * (D / 2), lane16 = piece * 16;
-      x.k = *reinterpret_cast<const uint4 *>(p + k_at + lane16);
-      x.v = *reinterpret_cast<const uint4 *>(p + w.v_off + k_at + lane16);
-      x.ks = (p + w.ks_off + slot * (D / 32))[piece];
-      if (scales) x.vs = (p + w.vs_off + slot)[lane & 31];
-    }
+    const uint32_t slot = unit_of(tile) & page_mask;
+    const uint8_t *const p = base + uint64_t(id < w.n_pages ? id : 0) * w.page_bytes;
+    const uint32_t k_at = slot * (D / 2), lane16 = piece * 16;
+    x.k = *reinterpret_cast<const uint4 *>(p + k_at + lane16);
+    x.v = *reinterpret_cast<const uint4 *>(p + w.v_off + k_at + lane16);
+    x.ks = (p + w.ks_off + slot * (D / 32))[piece];
+    x.vs = (p + w.vs_off + slot)[lane & 31];
     return x;
   };
   const uint32_t k_to = (unit * kUnit + piece / (D / 32)) * kRow + piece % (D / 32) * 16;
@@ -607,11 +607,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   const uint32_t krow = (col & 19) | (col >> 3 & 1) << 2 | (col >> 2 & 1) << 3;
   const uint32_t k_from = krow * kRow + 16 * half, v_from = kV + col * kVRow + 16 * half;
 
-  auto compute = [&](uint32_t tile, const uint8_t *buf) {
-    const int32_t at = int32_t(tile * kPromptTile);
-    if (at >= w_hi || at + int32_t(kPromptTile) <= w_lo) return;
-    const uint4 odd = *reinterpret_cast<const uint4 *>(buf + kOdd);  // gone, NaN of each unit
-    floatx16 sc[2];
+  // the scores of a tile
+  auto scores = [&](const uint8_t *buf, floatx16 (&x)[2]) {
     const int ks = *reinterpret_cast<const int *>(buf + kKS + lane * 4);
     auto keys = [&](int u, int kk) {
       return widen(*reinterpret_cast<const int4v *>(buf + k_from + u * kUnit * kRow + 32 * kk));
@@ -619,22 +616,25 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[u][i] = 0.0f;
-    {
-      const int8v k0 = keys(0, 0), k1 = keys(1, 0);
-      sc[0] = mul32<0>(k0, query.h[0], sc[0], ks, query.hs[0]);
-      sc[1] = mul32<2>(k1, query.h[0], sc[1], ks, query.hs[0]);
-      sc[0] = mul32<0>(k0, query.l[0], sc[0], ks, query.ls[0]);
-      sc[1] = mul32<2>(k1, query.l[0], sc[1], ks, query.ls[0]);
-    }
+      for (int i = 0; i < 16; ++i) x[u][i] = 0.0f;
+    const int8v k0 = keys(0, 0), k1 = keys(1, 0);
+    x[0] = mul32<0>(k0, query.h[0], x[0], ks, query.hs[0]);
+    x[1] = mul32<2>(k1, query.h[0], x[1], ks, query.hs[0]);
+    x[0] = mul32<0>(k0, query.l[0], x[0], ks, query.ls[0]);
+    x[1] = mul32<2>(k1, query.l[0], x[1], ks, query.ls[0]);
     if constexpr (KK == 2) {
-      const int8v k0 = keys(0, 1), k1 = keys(1, 1);
-      sc[0] = mul32<1>(k0, query.h[1], sc[0], ks, query.hs[1]);
-      sc[1] = mul32<3>(k1, query.h[1], sc[1], ks, query.hs[1]);
-      sc[0] = mul32<1>(k0, query.l[1], sc[0], ks, query.ls[1]);
-      sc[1] = mul32<3>(k1, query.l[1], sc[1], ks, query.ls[1]);
+      const int8v k2 = keys(0, 1), k3 = keys(1, 1);
+      x[0] = mul32<1>(k2, query.h[1], x[0], ks, query.hs[1]);
+      x[1] = mul32<3>(k3, query.h[1], x[1], ks, query.hs[1]);
+      x[0] = mul32<1>(k2, query.l[1], x[0], ks, query.ls[1]);
+      x[1] = mul32<3>(k3, query.l[1], x[1], ks, query.ls[1]);
     }
-    __builtin_amdgcn_s_setprio(1);  // ahead of the block's and the other block's products
+  };
+  // a tile's P and sums from its scores, and beside them the next tile's scores
+  auto compute = [&](uint32_t tile, const uint8_t *buf, const uint8_t *buf_next,
+                     floatx16 (&sc)[2]) {
+    const int32_t at = int32_t(tile * kPromptTile);
+    const uint4 odd = *reinterpret_cast<const uint4 *>(buf + kOdd);  // gone, NaN of each unit
     // masks, where some column does not see some token
     if (at + int32_t(kPromptTile) > all_hi || at < all_lo ||
         eq_dev::uniform(odd.x | odd.y | odd.z | odd.w) != 0) {
@@ -654,8 +654,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * a.c;
+    mx *= a.c;
     if (__any(mx > m_run)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
       const float m_new = mx > m_run ? mx + 8.0f : m_run;
       m_use = m_new == -INFINITY ? 0.0f : m_new;
       const float f = exp2_(m_run - m_use);
@@ -664,50 +665,104 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 #pragma unroll
       for (int m = 0; m < ND; ++m) o[m] *= f;
     }
-    uint4 p16[4];  // w P of 16 tokens each
+    // Eight steps, each with one product of the next tile's scores, four tokens
+    // of this tile's softmax for each column, and, two steps behind, half of the
+    // products of 16 tokens' values.  A step's operands are read from LDS in the
+    // step before.  The barriers keep the compiler from undoing that: a step's
+    // vector instructions run beside its matrix instructions.
+    floatx16 next[2];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      uint32_t pk[4];
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int j = 0; j < 8; j += 4) {
-        const floatx4 wt = *reinterpret_cast<const floatx4 *>(buf + kW + (16 * g + 8 * half + j) * 4);
-        float p[4];
+      for (int i = 0; i < 16; ++i) next[u][i] = 0.0f;
+    const int ks = *reinterpret_cast<const int *>(buf_next + kKS + lane * 4);
+    constexpr int kHalf = ND / 2;
+    int4v kf = *reinterpret_cast<const int4v *>(buf_next + k_from), kf_next = kf;
+    floatx4 wt = *reinterpret_cast<const floatx4 *>(buf + kW + 32 * half);
+    bf16x8 vf[kHalf], vf_next[kHalf];
+    uint32_t p16[4][4];  // w P of 16 tokens each
+    auto step = [&](auto ic) {
+      constexpr int I = decltype(ic)::value, G = I / 2, J = 4 * (I & 1);
+      floatx4 wt_next = wt;
+      if constexpr (I < 7)
+        wt_next = *reinterpret_cast<const floatx4 *>(buf + kW + (16 * ((I + 1) / 2) + 8 * half +
+                                                               4 * ((I + 1) & 1)) * 4);
+      if constexpr (I >= 1) {
+        constexpr int V = I - 1;  // the next step's values: 16 tokens V / 2, half V % 2
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          p[e] = exp2_(__builtin_fmaf(sc[g / 2][8 * (g & 1) + j + e], a.c, -m_use));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) l_run += p[e];
-        pk[j / 2] = eq_dev::pack_bf16(p[0] * wt[0], p[1] * wt[1]);
-        pk[j / 2 + 1] = eq_dev::pack_bf16(p[2] * wt[2], p[3] * wt[3]);
+        for (int m = 0; m < kHalf; ++m)
+          vf_next[m] = *reinterpret_cast<const bf16x8 *>(
+              buf + v_from + ((V & 1) * kHalf + m) * 32 * kVRow + 32 * (V / 2));
       }
-      p16[g] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-    }
-    __builtin_amdgcn_s_setprio(0);
+      if constexpr ((I & 1) == 1 && I < 4 * KK - 1) {
+        constexpr int K = (I + 1) / 2;  // the next key operand: unit K / KK, channels K % KK
+        kf_next = *reinterpret_cast<const int4v *>(buf_next + k_from + K / KK * kUnit * kRow +
+                                                   32 * (K % KK));
+      }
+      if constexpr (I < 4 * KK) {
+        constexpr int K = I / 2, U = K / KK, C = K % KK;
+        next[U] = mul32<2 * U + C>(widen(kf), I & 1 ? query.l[C] : query.h[C], next[U], ks,
+                                   I & 1 ? query.ls[C] : query.hs[C]);
+      }
+      if constexpr (I >= 2) {
+        constexpr int V = I - 2;
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+        for (int m = 0; m < kHalf; ++m) {
+          constexpr int at = (V & 1) * kHalf;
+          o[at + m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              vf[m], __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4 *>(p16[V / 2])), o[at + m],
+              0, 0, 0);
+        }
+      }
+      float p[4];
 #pragma unroll
-      for (int m = 0; m < ND; ++m)
-        o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            *reinterpret_cast<const bf16x8 *>(buf + v_from + m * 32 * kVRow + 32 * g),
-            __builtin_bit_cast(bf16x8, p16[g]), o[m], 0, 0, 0);
+      for (int e = 0; e < 4; ++e)
+        p[e] = exp2_(__builtin_fmaf(sc[G / 2][8 * (G & 1) + J + e], a.c, -m_use));
+      l_run += (p[0] + p[1]) + (p[2] + p[3]);
+      p16[G][J / 2] = eq_dev::pack_bf16(p[0] * wt[0], p[1] * wt[1]);
+      p16[G][J / 2 + 1] = eq_dev::pack_bf16(p[2] * wt[2], p[3] * wt[3]);
+      wt = wt_next;
+      if constexpr ((I & 1) == 1) kf = kf_next;
+#pragma unroll
+      for (int m = 0; m < kHalf; ++m) vf[m] = vf_next[m];
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    __builtin_amdgcn_sched_barrier(0);
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
+    step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 5>{});
+    step(std::integral_constant<int, 6>{});
+    step(std::integral_constant<int, 7>{});
+#pragma unroll
+    for (int m = 0; m < ND; ++m)
+      o[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          m < kHalf ? vf[m] : *reinterpret_cast<const bf16x8 *>(buf + v_from + m * 32 * kVRow + 96),
+          __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4 *>(p16[3])), o[m], 0, 0, 0);
+    sc[0] = next[0], sc[1] = next[1];
   };
 
   const uint32_t t0 = sp.first + chunk * a.chunk_tiles, t1 = min(t0 + a.chunk_tiles, sp.last);
   if (t0 < t1) {
-    uint32_t id = load_id(t0);
-    store_tile(lds, t0, load_tile(t0, id));
-    id = load_id(t0 + 1);
+    const bool active = wave_col < sp.cols;
+    floatx16 sc[2];
+    uint8_t *now = lds, *next = lds + kBuf, *then = lds + 2 * kBuf;
+    store_tile(now, t0, load_tile(t0, load_id(t0)));
+    if (t0 + 1 < t1) store_tile(next, t0 + 1, load_tile(t0 + 1, load_id(t0 + 1)));
+    uint32_t id = load_id(t0 + 2);
     __syncthreads();
+    if (active) scores(now, sc);
     for (uint32_t t = t0; t < t1; ++t) {
-      Stage x{};
-      const bool more = t + 1 < t1;
-      if (more) {
-        x = load_tile(t + 1, id);
-        id = load_id(t + 2);
-      }
-      compute(t, lds + ((t - t0) & 1) * kBuf);
-      if (more) store_tile(lds + ((t + 1 - t0) & 1) * kBuf, t + 1, x);
+      const bool more = t + 2 < t1;
+      const Stage x = load_tile(t + 2, id);
+      id = load_id(t + 3);
+      if (active) compute(t, now, next, sc);  // (behind the last tile: scores of anything)
+      if (more) store_tile(then, t + 2, x);
       __syncthreads();
+      uint8_t *const old = now;
+      now = next, next = then, then = old;
     }
   }
   l_run += __shfl_xor(l_run, 32);
