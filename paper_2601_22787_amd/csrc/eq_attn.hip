@@ -79,7 +79,7 @@ __device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
   p.seen = uint32_t(end_of(q, pos1));
   p.first = uint32_t(start_of(a.window, pos0)) / TILE;
   p.last = max((p.seen + TILE - 1) / TILE, p.first);
-  p.chunks = (p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles;
+  p.chunks = min((p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles, a.chunks);
   return p;
 }
 
@@ -119,34 +119,39 @@ template <int D>
 struct Query {
   int8v h, l;
   int hs, ls;
-  __device__ inline void load(const uint16_t *row, uint32_t col, uint32_t g) {
-    float x[32];
-    auto half = [&](int at, uint32_t ch) {
-      uint32_t u[8] = {};
-      if (row) {
-        *reinterpret_cast<uint4 *>(u) = *reinterpret_cast<const uint4 *>(row + ch);
-        *reinterpret_cast<uint4 *>(u + 4) = *reinterpret_cast<const uint4 *>(row + ch + 8);
-      }
+  // a lane's channels of `row` (zeros where that is null)
+  __device__ inline void read(const uint16_t *row, uint32_t g, uint32_t (&raw)[D / 8]) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) raw[i] = 0;
+    if (!row) return;
+#pragma unroll
+    for (int i = 0; i < D / 8; i += 4)
+      *reinterpret_cast<uint4 *>(raw + i) =
+          *reinterpret_cast<const uint4 *>(row + i / 8 * 64 + 16 * g + i % 8 * 2);
+  }
+  __device__ inline void split(const uint32_t (&raw)[D / 8], uint32_t col, uint32_t g) {
+    float x[D / 4];
+    int byte[D / 64];
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) {
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[at + 2 * i] = __uint_as_float(u[i] << 16);
-        x[at + 2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-        top = max(top, max(u[i] << 16 & 0x7FFFFFFFu, u[i] & 0x7FFF0000u));
+      for (int i = 8 * k; i < 8 * k + 8; ++i) {
+        x[2 * i] = __uint_as_float(raw[i] << 16);
+        x[2 * i + 1] = __uint_as_float(raw[i] & 0xFFFF0000u);
+        top = max(top, max(raw[i] << 16 & 0x7FFFFFFFu, raw[i] & 0x7FFF0000u));
       }
-      return top_byte(max(top, uint32_t(__shfl_xor(int(top), 16))));
-    };
-    const int a = half(0, 16 * g);
-    const int from_a = __shfl(a, int(32 * (g & 1) + col));
+      byte[k] = top_byte(max(top, uint32_t(__shfl_xor(int(top), 16))));
+    }
+    const int from_a = __shfl(byte[0], int(32 * (g & 1) + col));
     if constexpr (D == 128) {
-      const int b = half(16, 64 + 16 * g);
-      const int from_b = __shfl(b, int(32 * (g & 1) + col));
+      const int from_b = __shfl(byte[1], int(32 * (g & 1) + col));
       hs = g < 2 ? from_a : from_b;
       ls = low_byte(hs);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        int u, v;
-        split4(x + 4 * i, byte_value(i < 4 ? a : b), u, v);
+        int u = 0, v = 0;
+        split4(x + 4 * i, byte_value(byte[i / 4]), u, v);
         h[i] = u;
         l[i] = v;
       }
@@ -155,8 +160,8 @@ struct Query {
       ls = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        int u, v;
-        split4(x + 4 * i, byte_value(a), u, v);
+        int u = 0, v = 0;
+        split4(x + 4 * i, byte_value(byte[0]), u, v);
         h[i] = u;
         h[4 + i] = v;
       }
@@ -176,6 +181,21 @@ __device__ inline uint32_t code_pair(uint32_t codes) {
 template <int BYTE>
 __device__ inline floatx16 mul32(int8v codes, int8v terms, floatx16 acc, int as, int bs) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes, terms, acc, 4, 0, BYTE, as, 0, bs);
+}
+
+// acc + codes x terms: 16 x 16 over 128 steps, the codes' scales in byte BYTE of as.
+template <int BYTE>
+__device__ inline floatx4 mul16(int8v codes, int8v terms, floatx4 acc, int as, int bs) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes, terms, acc, 4, 0, BYTE, as, 0, bs);
+}
+
+// All ones where bit i of m is set, else 0.
+__device__ inline uint32_t bit_mask(uint32_t m, int i) { return uint32_t(int32_t(m << (31 - i)) >> 31); }
+
+// The largest x of the four lanes (col, g) of a column.
+__device__ inline float column_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
 }
 
 // One block: kCols query columns of a key/value head against a chunk of token
@@ -199,12 +219,38 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const uint32_t s = blockIdx.y;
   const uint32_t chunk = blockIdx.x % a.chunks, rest = blockIdx.x / a.chunks;
   const uint32_t qt = rest % a.q_tiles, h = rest / a.q_tiles;
-  const Seq q = sequence(w, s);
   const uint32_t col0 = qt * kCols;
-  const Span sp = span_of<kCols, kTile>(a, q, col0);
-  if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
   const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
   const uint32_t col = lane & 15, g = lane >> 4;
+  const Seq q = sequence(w, s);
+  const Span sp = span_of<kCols, kTile>(a, q, col0);
+
+  // Page numbers of a tile's four 32-token units (one page when it holds them
+  // all), by scalar loads.  The table is read up to its width, not up to the
+  // sequence's length, so that the first ones need not wait for that; what they
+  // name beyond it is masked.
+  const int32_t *const table = w.page_table + size_t(s) * w.max_pages;
+  const uint32_t page_mask = (1u << w.page_shift) - 1;
+  const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
+  struct Ids {
+    uint32_t u[ONE ? 1 : 4];
+  };
+  auto load_ids = [&](uint32_t tile) {
+    Ids d;
+#pragma unroll
+    for (uint32_t u = 0; u < (ONE ? 1 : 4); ++u)
+      d.u[u] = eq_dev::as_const(table)[min((tile * 4 + u) * kUnit >> w.page_shift, w.max_pages - 1)];
+    return d;
+  };
+  uint32_t first = 0;
+  if (a.window) first = sp.first;
+  uint32_t t = first + chunk * a.chunk_tiles + wave;
+  Ids ids = load_ids(t);
+  if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
+  const uint32_t t_end = min(sp.first + (chunk + 1) * a.chunk_tiles, sp.last);
+  // the wavefront's last tile, which is loaded again where there is no next one
+  // (loads under a condition would be waited for where the branches meet)
+  const uint32_t t_last = t < t_end ? t + (t_end - 1 - t) / kWaves * kWaves : t;
 
   // this lane's column
   const uint32_t index = col0 + col;
@@ -212,187 +258,168 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const uint32_t token = index / a.group;
   const int32_t pos = q.base + int32_t(token);
   const int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
-  Query<D> query;
-  query.load(real ? a.q + uint64_t(q.row + token) * a.q_stride +
-                        uint64_t(h * a.group + index % a.group) * D
-                  : nullptr,
-             col, g);
 
-  const uint32_t t_end = min(sp.first + (chunk + 1) * a.chunk_tiles, sp.last);
-  uint32_t t = sp.first + chunk * a.chunk_tiles + wave;
-
-  // addresses: the four 32-token units of a tile may be in four pages
-  const int32_t *const table = w.page_table + size_t(s) * w.max_pages;
-  const uint32_t last_unit = sp.seen ? (sp.seen - 1) / kUnit : 0;
-  const uint32_t page_mask = (1u << w.page_shift) - 1;
-  const uint8_t *const base = w.pages + uint64_t(h) * w.head_bytes;
-  auto first_token = [&](uint32_t tile, uint32_t unit) {
-    return min(tile * 4 + unit, last_unit) * kUnit;
-  };
-  struct Ids {
-    int ka, kb, v, sa, sb;
-  };
-  const uint32_t gk = (lane & 15) >> 2, r = lane & 3;
-  auto load_ids = [&](uint32_t tile) {
-    Ids d;
-    if constexpr (ONE) {
-      d.ka = table[first_token(tile, 0) >> w.page_shift];
-      d.kb = d.v = d.sa = d.sb = d.ka;
-    } else {
-      d.ka = table[first_token(tile, gk >> 1) >> w.page_shift];
-      d.kb = table[first_token(tile, 2 + (gk >> 1)) >> w.page_shift];
-      d.v = table[first_token(tile, g) >> w.page_shift];
-      d.sa = table[first_token(tile, g >> 1) >> w.page_shift];
-      d.sb = table[first_token(tile, 2 + (g >> 1)) >> w.page_shift];
+  // a lane's parts of a tile: keys of units gk/2 and 2 + gk/2, values of unit g,
+  // value scales of units g/2 and 2 + g/2
+  const uint32_t gk = col >> 2, r = lane & 3, kg = D == 128 ? g : g & 1;
+  auto part_of = [&](const Ids &d, uint32_t unit) {
+    uint32_t id = d.u[0];
+    if constexpr (!ONE) {
+      const uint32_t low = unit & 1 ? d.u[1] : d.u[0], high = unit & 1 ? d.u[3] : d.u[2];
+      id = unit & 2 ? high : low;
     }
-    return d;
+    return base + uint64_t(id < w.n_pages ? id : 0) * w.page_bytes;
   };
-  auto part_of = [&](int id) {
-    return base + (uint32_t(id) < w.n_pages ? uint64_t(uint32_t(id)) : 0) * w.page_bytes;
-  };
-  auto slot_of = [&](uint32_t tile, uint32_t unit) { return first_token(tile, unit) & page_mask; };
-
+  auto slot_of = [&](uint32_t tile, uint32_t unit) { return (tile * 4 + unit) * kUnit & page_mask; };
   int4v kreg[8], vreg[ND];
   uint4 va, vb;
   int ksa, ksb;
-  const uint32_t kg = D == 128 ? g : g & 1;
   auto load_k = [&](uint32_t tile, const Ids &d) {
-    const uint8_t *const pa = part_of(d.ka), *const pb = part_of(d.kb);
+    const uint8_t *const pa = part_of(d, gk >> 1), *const pb = part_of(d, 2 + (gk >> 1));
     const uint32_t a0 = slot_of(tile, gk >> 1) + 16 * (gk & 1);
     const uint32_t b0 = slot_of(tile, 2 + (gk >> 1)) + 16 * (gk & 1);
-    const uint8_t *const ra = pa + (a0 + r) * (D / 2) + 16 * kg;
-    const uint8_t *const rb = pb + (b0 + r) * (D / 2) + 16 * kg;
+    const uint32_t at = r * (D / 2) + 16 * kg, ks_at = w.ks_off + (r * (D / 32) + kg) * 4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      kreg[i] = *reinterpret_cast<const int4v *>(ra + i * 2 * D);
-      kreg[4 + i] = *reinterpret_cast<const int4v *>(rb + i * 2 * D);
+      kreg[i] = *reinterpret_cast<const int4v *>(pa + (a0 * (D / 2) + at + i * 2 * D));
+      kreg[4 + i] = *reinterpret_cast<const int4v *>(pb + (b0 * (D / 2) + at + i * 2 * D));
     }
-    ksa = *reinterpret_cast<const int *>(pa + w.ks_off + a0 / 16 * (D / 2) + (r * (D / 32) + kg) * 4);
-    ksb = *reinterpret_cast<const int *>(pb + w.ks_off + b0 / 16 * (D / 2) + (r * (D / 32) + kg) * 4);
+    ksa = *reinterpret_cast<const int *>(pa + (ks_at + a0 * (D / 32)));
+    ksb = *reinterpret_cast<const int *>(pb + (ks_at + b0 * (D / 32)));
   };
   auto load_vs = [&](uint32_t tile, const Ids &d) {
-    va = *reinterpret_cast<const uint4 *>(part_of(d.sa) + w.vs_off + slot_of(tile, g >> 1) +
-                                          16 * (g & 1));
-    vb = *reinterpret_cast<const uint4 *>(part_of(d.sb) + w.vs_off + slot_of(tile, 2 + (g >> 1)) +
-                                          16 * (g & 1));
+    const uint32_t at = w.vs_off + 16 * (g & 1);
+    va = *reinterpret_cast<const uint4 *>(part_of(d, g >> 1) + (at + slot_of(tile, g >> 1)));
+    vb = *reinterpret_cast<const uint4 *>(part_of(d, 2 + (g >> 1)) + (at + slot_of(tile, 2 + (g >> 1))));
   };
   auto load_v = [&](uint32_t tile, const Ids &d) {
-    const uint8_t *const p = part_of(d.v) + w.v_off +
-                             (slot_of(tile, g) / kUnit * D + (lane & 15)) * 16;
+    const uint8_t *const p = part_of(d, g) + (w.v_off + slot_of(tile, g) * (D / 2) + col * 16);
 #pragma unroll
     for (int m = 0; m < ND; ++m) vreg[m] = *reinterpret_cast<const int4v *>(p + m * 256);
   };
 
-  float m_run = -INFINITY, l_run = 0.0f;
+  float m_run = -INFINITY, m_use = 0.0f, l_run = 0.0f;
+  int8v ph{}, pq{};  // w P of a tile, as two terms
   floatx4 o[ND];
 #pragma unroll
   for (int m = 0; m < ND; ++m) o[m] = floatx4{0, 0, 0, 0};
 
-  Ids cur{}, next{};
   if (t < t_end) {
-    cur = load_ids(t);
-    next = load_ids(t + kWaves);
-    load_k(t, cur);
-    load_vs(t, cur);
-    load_v(t, cur);
-  }
-  for (; t < t_end; t += kWaves) {
-    const bool more = t + kWaves < t_end;
-    floatx4 sc[8];
+    Query<D> query;
+    const uint16_t *const row =
+        real ? a.q + uint64_t(q.row + token) * a.q_stride + uint64_t(h * a.group + index % a.group) * D
+             : nullptr;
+    uint32_t raw[D / 8];
+    query.read(row, g, raw);
+    load_k(t, ids);
+    load_vs(t, ids);
+    load_v(t, ids);
+    Ids next = load_ids(min(t + kWaves, t_last));
+    query.split(raw, col, g);
+    for (; t < t_end; t += kWaves) {
+      const uint32_t t_next = min(t + kWaves, t_last);
+      floatx4 sc[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int8v k8 = widen(kreg[i]);
-      const int ks = i < 4 ? ksa : ksb;
-      sc[i] = floatx4{0, 0, 0, 0};
-      auto mul = [&](int8v b, int bs) {
-        switch (i & 3) {
-          case 0: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 0, ks, 0, bs); break;
-          case 1: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 1, ks, 0, bs); break;
-          case 2: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 2, ks, 0, bs); break;
-          default: sc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, b, sc[i], 4, 0, 3, ks, 0, bs); break;
-        }
-      };
-      mul(query.h, query.hs);
-      if constexpr (D == 128) mul(query.l, query.ls);
-    }
-    const bool bad_a = uint32_t(cur.sa) >= w.n_pages, bad_b = uint32_t(cur.sb) >= w.n_pages;
-    Ids after = next;
-    if (more) {
-      after = load_ids(t + 2 * kWaves);
-      load_k(t + kWaves, next);
-    }
-    // masks, only where some column does not see the whole tile
-    const int32_t at = int32_t(t * kTile);
-    uint32_t visible = 0;  // bit 4 i + r: this lane's column sees that token
-    const bool masked = at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || __any(bad_a || bad_b);
-    if (masked) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int32_t tok = at + 64 * (i / 4) + 16 * int32_t(g) + 4 * (i % 4) + e;
-          const bool ok = tok >= lo && tok < hi && !(i < 4 ? bad_a : bad_b);
-          visible |= uint32_t(ok) << (4 * i + e);
-          if (!ok) sc[i][e] = -INFINITY;
-        }
-    }
-    float mx = sc[0][0];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, sc[i][e]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float m_new = fmaxf(m_run, mx * a.c);
-    const float m_use = m_new == -INFINITY ? 0.0f : m_new;
-    if (__any(m_new > m_run)) {
-      const float f = exp2_(m_run - m_use);
-      l_run *= f;
-#pragma unroll
-      for (int m = 0; m < ND; ++m) o[m] *= f;
-      m_run = m_new;
-    }
-    float y[32];
-    float top = 0.0f;
-    const uint32_t vs[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = exp2_(__builtin_fmaf(sc[i][e], a.c, -m_use));
-        l_run += p;
-        y[4 * i + e] = p * __uint_as_float((vs[i] >> (8 * e) & 255u) << 23);
+      for (int i = 0; i < 8; ++i) {
+        const int8v k8 = widen(kreg[i]);
+        const int ks = i < 4 ? ksa : ksb;
+        sc[i] = floatx4{0, 0, 0, 0};
+        auto mul = [&](int8v b, int bs) {
+          switch (i & 3) {
+            case 0: sc[i] = mul16<0>(k8, b, sc[i], ks, bs); break;
+            case 1: sc[i] = mul16<1>(k8, b, sc[i], ks, bs); break;
+            case 2: sc[i] = mul16<2>(k8, b, sc[i], ks, bs); break;
+            default: sc[i] = mul16<3>(k8, b, sc[i], ks, bs); break;
+          }
+        };
+        mul(query.h, query.hs);
+        if constexpr (D == 128) mul(query.l, query.ls);
       }
-    if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
+      load_k(t_next, next);
+      // masks, where some column does not see the whole tile
+      const int32_t at = int32_t(t * kTile);
+      uint32_t gone = 0;  // bit u: unit u's page is not there
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (!(visible >> i & 1)) y[i] = 0.0f;
+      for (uint32_t u = 0; u < (ONE ? 1 : 4); ++u) gone |= uint32_t(ids.u[u] >= w.n_pages) << u;
+      if (ONE && gone) gone = 15;
+      const bool masked = at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || gone;
+      uint32_t visible = ~0u;  // bit 4 i + e: this lane's column sees that token
+      if (masked) {
+        auto bits = [&](uint32_t unit, int32_t from) {  // of 16 tokens
+          const int32_t x = min(max(lo - from, 0), 16), y = min(max(hi - from, x), 16);
+          return gone >> unit & 1 ? 0u : (1u << y) - (1u << x);
+        };
+        visible = bits(g >> 1, at + 16 * int32_t(g)) | bits(2 + (g >> 1), at + 64 + 16 * int32_t(g)) << 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sc[i][e] = __uint_as_float((__float_as_uint(sc[i][e]) & bit_mask(visible, 4 * i + e)) |
+                                       (0xFF800000u & ~bit_mask(visible, 4 * i + e)));
+      }
+      // The maximum is set 8 above the scores and follows when they reach it: a
+      // lane then compares its own 32, and the four that share a column seldom
+      // have to agree on a new one.
+      float part[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        part[k] = sc[2 * k][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) part[k] = fmaxf(part[k], sc[2 * k + i / 4][i % 4]);
+      }
+      float mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * a.c;
+      if (__any(mx > m_run)) {
+        mx = column_max(mx);
+        const float m_new = mx > m_run ? mx + 8.0f : m_run;
+        m_use = m_new == -INFINITY ? 0.0f : m_new;
+        const float f = exp2_(m_run - m_use);
+        l_run *= f;
+#pragma unroll
+        for (int m = 0; m < ND; ++m) o[m] *= f;
+        m_run = m_new;
+      }
+      float y[32];
+      const uint32_t vs[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = exp2_(__builtin_fmaf(sc[i][e], a.c, -m_use));
+        l_run += (p[0] + p[1]) + (p[2] + p[3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          y[4 * i + e] = p[e] * __uint_as_float((vs[i] >> (8 * e) & 255u) << 23);
+      }
+      if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          y[i] = __uint_as_float(__float_as_uint(y[i]) & bit_mask(visible, i));
+      }
+      float top = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
+      load_vs(t_next, next);
+      top = column_max(top);
+      const int ps = top_byte(__float_as_uint(top));
+      const int pl = low_byte(ps);
+      const float scale = byte_value(ps);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        int u = ph[i], v = pq[i];
+        split4(y + 4 * i, scale, u, v);
+        ph[i] = u;
+        pq[i] = v;
+      }
+#pragma unroll
+      for (int m = 0; m < ND; ++m) {
+        const int8v v8 = widen(vreg[m]);
+        o[m] = mul16<0>(v8, ph, o[m], kUnitScale, ps);
+        o[m] = mul16<0>(v8, pq, o[m], kUnitScale, pl);
+      }
+      load_v(t_next, next);
+      ids = next;
+      next = load_ids(min(t_next + kWaves, t_last));
     }
-#pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
-    if (more) load_vs(t + kWaves, next);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const int ps = top_byte(__float_as_uint(top));
-    const int pl = low_byte(ps);
-    const float scale = byte_value(ps);
-    int8v ph, pq;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      int u, v;
-      split4(y + 4 * i, scale, u, v);
-      ph[i] = u;
-      pq[i] = v;
-    }
-#pragma unroll
-    for (int m = 0; m < ND; ++m) {
-      const int8v v8 = widen(vreg[m]);
-      o[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8, ph, o[m], 4, 0, 0, kUnitScale, 0, ps);
-      o[m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8, pq, o[m], 4, 0, 0, kUnitScale, 0, pl);
-    }
-    if (more) load_v(t + kWaves, next);
-    cur = next;
-    next = after;
   }
   l_run += __shfl_xor(l_run, 16);
   l_run += __shfl_xor(l_run, 32);
@@ -409,10 +436,10 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   float m_all = -INFINITY, l_all = 0.0f, sum[kPer] = {};
 #pragma unroll
   for (uint32_t v = 0; v < kWaves; ++v) m_all = fmaxf(m_all, lds_s[v][oc].x);
-  const float m_use = m_all == -INFINITY ? 0.0f : m_all;
+  const float m_ref = m_all == -INFINITY ? 0.0f : m_all;
 #pragma unroll
   for (uint32_t v = 0; v < kWaves; ++v) {
-    const float f = exp2_(lds_s[v][oc].x - m_use);
+    const float f = exp2_(lds_s[v][oc].x - m_ref);
     l_all += f * lds_s[v][oc].y;
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i) sum[i] += f * lds_o[(v * kCols + oc) * kStride + d0 + i];
@@ -792,13 +819,13 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
           floatx4{o[m][i], o[m][i + 1], o[m][i + 2], o[m][i + 3]};
 }
 
-// Joins the chunks of one query head at one new token, a block each: 8
-// sub-blocks of threads take the chunks in turn, then add up through LDS.
+// Joins the chunks of one query head at one new token, a block each: every
+// wavefront takes all chunks' maxima and sums, a lane each, and 8 groups of
+// threads the chunks' O in turn, added up through LDS.
 template <int D, uint32_t COLS, uint32_t TILE>
 __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   constexpr uint32_t kLanes = D / 4, kSub = 8;
   __shared__ __attribute__((aligned(16))) float4 lds[kSub][kLanes];
-  __shared__ float lds_l[kSub];
   const View &w = a.w;
   const uint32_t s = blockIdx.y, heads = w.kv_heads * a.group;
   const uint32_t token = blockIdx.x / heads, head = blockIdx.x % heads;
@@ -810,30 +837,46 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   if (sp.chunks <= 1) return;
   const uint64_t first =
       (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * COLS + index % COLS;
+  const uint32_t sub = threadIdx.x / kLanes, l = threadIdx.x % kLanes, lane = threadIdx.x & 63;
   float m = -INFINITY;
-  for (uint32_t c = 0; c < sp.chunks; ++c) m = fmaxf(m, a.stat[first + uint64_t(c) * COLS].x);
+  float2 st = make_float2(-INFINITY, 0.0f);
+  for (uint32_t c0 = 0; c0 < sp.chunks; c0 += 64) {
+    st = c0 + lane < sp.chunks ? a.stat[first + uint64_t(c0 + lane) * COLS] : make_float2(-INFINITY, 0.0f);
+    m = fmaxf(m, st.x);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
   if (m == -INFINITY) m = 0.0f;
-  const uint32_t sub = threadIdx.x / kLanes, l = threadIdx.x % kLanes;
   float4 o = make_float4(0, 0, 0, 0);
   float total = 0.0f;
-#pragma unroll 4
-  for (uint32_t c = sub; c < sp.chunks; c += kSub) {
-    const uint64_t at = first + uint64_t(c) * COLS;
-    const float2 st = a.stat[at];
-    const float4 x = *reinterpret_cast<const float4 *>(a.part + at * D + 4 * l);
+  for (uint32_t c0 = 0; c0 < sp.chunks; c0 += 64) {
+    if (sp.chunks > 64)
+      st = c0 + lane < sp.chunks ? a.stat[first + uint64_t(c0 + lane) * COLS] : make_float2(-INFINITY, 0.0f);
     const float f = exp2_(st.x - m);
     total += f * st.y;
-    o.x += f * x.x, o.y += f * x.y, o.z += f * x.z, o.w += f * x.w;
+    const uint32_t n = min(sp.chunks - c0, 64u);
+    for (uint32_t k = 0; k * kSub < n; k += 4) {  // (as often for every lane)
+      float4 x[4];
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        x[j] = *reinterpret_cast<const float4 *>(
+            a.part + (first + uint64_t(c0 + min(sub + (k + j) * kSub, n - 1)) * COLS) * D + 4 * l);
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        const float fc = __shfl(f, int(sub + (k + j) * kSub));  // 0 behind the last chunk
+        o.x += fc * x[j].x, o.y += fc * x[j].y, o.z += fc * x[j].z, o.w += fc * x[j].w;
+      }
+    }
   }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
   lds[sub][l] = o;
-  if (l == 0) lds_l[sub] = total;
   __syncthreads();
   if (sub) return;
 #pragma unroll
   for (uint32_t i = 1; i < kSub; ++i) {
     const float4 x = lds[i][l];
     o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
-    total += lds_l[i];
   }
   const float inv = total == 0.0f ? 0.0f : 1.0f / total;
   *reinterpret_cast<uint2 *>(a.out + (uint64_t(q.row + token) * heads + head) * D + 4 * l) =
@@ -852,9 +895,10 @@ struct Plan {
 };
 
 constexpr uint32_t kFewCols = 64;
+constexpr uint32_t kWholeTiles = 16;
 
 Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_new,
-               uint32_t max_len) {
+               uint32_t max_len, uint32_t window) {
   Plan p;
   const uint64_t cols = uint64_t(max_new) * group;
   p.prompt = cols > kFewCols;
@@ -864,11 +908,22 @@ Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_
   const uint64_t work = uint64_t(n_seqs) * kv_heads * p.q_tiles;
   const uint32_t tiles = (max_len + p.tile - 1) / p.tile;
   const uint64_t want = std::max<uint64_t>(1, (512 + work - 1) / work);
-  uint32_t ct = uint32_t((tiles + want - 1) / want);
-  ct = std::max((ct + 3) / 4 * 4, 4u);
+  auto round4 = [](uint64_t v) { return uint32_t(std::max<uint64_t>((v + 3) / 4 * 4, 4)); };
+  uint32_t ct = round4((tiles + want - 1) / want);
   if (work < (p.prompt ? 512 : 2048)) ct = std::min(ct, 4096 / p.tile);
-  p.chunk_tiles = ct;
+  if (!p.prompt && tiles <= kWholeTiles) ct = round4(tiles);
   p.chunks = std::max((tiles + ct - 1) / ct, 1u);
+  // a window leaves fewer tiles (a query's window and the others' of its
+  // sequence), in at most as many chunks: the workspace does not depend on it
+  uint32_t seen = tiles;
+  if (window)
+    seen = uint32_t(std::min<uint64_t>(tiles, (uint64_t(window) + max_new + p.tile - 2) / p.tile + 1));
+  if (seen < tiles) {
+    ct = round4((seen + p.chunks - 1) / p.chunks);
+    if (!p.prompt && seen <= kWholeTiles) ct = round4(seen);
+    p.chunks = std::max((seen + ct - 1) / ct, 1u);
+  }
+  p.chunk_tiles = ct;
   return p;
 }
 
@@ -909,7 +964,7 @@ extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq
       batch->max_new == 0)
     return 0;
   return attn_bytes(plan_attn(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads,
-                              batch->max_new, batch->max_len),
+                              batch->max_new, batch->max_len, 0),
                     cache, batch);
 }
 
@@ -923,7 +978,8 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
       q_stride % 8 || (batch->n_tokens > 1 && q_stride < uint64_t(q_heads) * cache->head_dim))
     return EQ_EINVAL;
   const uint32_t group = q_heads / cache->kv_heads;
-  const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len);
+  const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len,
+                           window);
   const size_t need = attn_bytes(p, cache, batch);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return EQ_EINVAL;
   const uint64_t blocks = uint64_t(cache->kv_heads) * p.q_tiles * p.chunks;

@@ -38,8 +38,7 @@ inline bool batch_ok(const eq_kv_cache *c, const eq_kv_batch *b) {
          c->n_pages <= 0x7FFFFFFFu && b->n_seqs <= 65535 && b->max_new <= b->n_tokens &&
          b->n_tokens <= 1u << 30 && b->max_len <= 1u << 30 &&
          b->max_len <= uint64_t(b->max_pages) * c->page_tokens &&
-         (b->n_seqs == 0 || (b->seq_start && b->kv_len)) &&
-         (b->n_seqs == 0 || b->max_pages == 0 || b->page_table);
+         (b->n_seqs == 0 || (b->seq_start && b->kv_len && b->page_table && b->max_pages >= 1));
 }
 
 inline View view(const eq_kv_cache *c, const eq_kv_batch *b) {

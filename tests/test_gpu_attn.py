@@ -226,26 +226,27 @@ def test_strided_queries_and_another_stream(eq):
     check(out.double().cpu().numpy(), q.double().cpu().numpy(), k, v, news, lens, 0.125, 0)
 
 
-def test_graph_of_a_generation_step(eq):
+@pytest.mark.parametrize("max_len", [1280, 5120])  # one chunk a sequence, several
+def test_graph_of_a_generation_step(eq, max_len):
     """Norm and rotation, append and attention captured once, at the sizes that
     bound the run, and replayed as the sequences grow, with eager work between;
     every replay equals the eager calls bit for bit."""
     hq, hk, dim, page, n = 8, 2, 128, 32, 3
-    start_lens = [30, 1200, 0]
-    table = dev(np.random.default_rng(0).permutation(3 * 40).reshape(3, 40).astype(np.int32))
+    start_lens, wide = [30, max_len - 80, 0], max_len // 32
+    table = dev(np.random.default_rng(0).permutation(3 * wide).reshape(3, wide).astype(np.int32))
     lens = torch.tensor(start_lens, dtype=torch.int32, device="cuda")
     pos = torch.empty(3, dtype=torch.int32, device="cuda")
     starts = torch.arange(n + 1, dtype=torch.int32, device="cuda")
-    cos, sin = tables(1280, dim // 2)
+    cos, sin = tables(max_len, dim // 2)
     rope = eq.Rope(dev(cos), dev(sin))
     w = torch.randn(dim, device="cuda").to(torch.bfloat16)
-    b = eq.KvBatch(starts, lens, table, n_tokens=n, max_new=1, max_len=1280)
+    b = eq.KvBatch(starts, lens, table, n_tokens=n, max_new=1, max_len=max_len)
     xq, xk, xv = (torch.randn(n, h, dim, device="cuda") for h in (hq, hk, hk))
 
     def state():
         g = torch.Generator(device="cuda")
         g.manual_seed(1)
-        c = eq.KvCache.empty(120, page_tokens=page, kv_heads=hk, head_dim=dim)
+        c = eq.KvCache.empty(3 * wide, page_tokens=page, kv_heads=hk, head_dim=dim)
         c.pages.copy_(torch.randint(0, 120, c.pages.shape, device="cuda", generator=g))
         return c, [torch.empty(n, h, dim, dtype=torch.bfloat16, device="cuda") for h in (hq, hk, hq)]
 
@@ -257,7 +258,7 @@ def test_graph_of_a_generation_step(eq):
     ca, oa = state()
     cb, ob = state()
     wsa, wsb = eq.attn_workspace(ca, b, hq), eq.attn_workspace(cb, b, hq)
-    assert wsa is not None
+    assert (wsa is not None) == (max_len == 5120)
     pos.copy_(lens)
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
@@ -274,7 +275,8 @@ def test_graph_of_a_generation_step(eq):
         xq.normal_(), xk.normal_(), xv.normal_()
         for o in oa:
             o.fill_(float("nan"))
-        wsa.fill_(255)
+        if wsa is not None:
+            wsa.fill_(255)
         g.replay()
         step(cb, ob, wsb)
         torch.cuda.synchronize()
