@@ -198,6 +198,13 @@ __device__ inline float column_max(float x) {
   return fmaxf(x, __shfl_xor(x, 32));
 }
 
+// 32 codes; STREAM: which nothing reads again before the caches are full of others.
+template <bool STREAM>
+__device__ inline int4v load_codes(const uint8_t *p) {
+  const int4v *const v = reinterpret_cast<const int4v *>(p);
+  return STREAM ? __builtin_nontemporal_load(v) : *v;
+}
+
 // One block: kCols query columns of a key/value head against a chunk of token
 // tiles, dealt to its 4 wavefronts in turn; each keeps its own maximum, sum and
 // O, joined through LDS at the end.
@@ -209,7 +216,7 @@ __device__ inline float column_max(float x) {
 // Then a lane's 32 scores are the 32 tokens of its steps in order, and P passes
 // from the first product to the second without leaving the lane.  V lies along
 // the tokens in the cache, 32 to a 16-byte row, as the second product takes it.
-template <int D, bool ONE>
+template <int D, bool ONE, bool STREAM>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int ND = D / 16;
   constexpr uint32_t kStride = D + 4;  // floats a column in LDS
@@ -281,8 +288,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     const uint32_t at = r * (D / 2) + 16 * kg, ks_at = w.ks_off + (r * (D / 32) + kg) * 4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      kreg[i] = *reinterpret_cast<const int4v *>(pa + (a0 * (D / 2) + at + i * 2 * D));
-      kreg[4 + i] = *reinterpret_cast<const int4v *>(pb + (b0 * (D / 2) + at + i * 2 * D));
+      kreg[i] = load_codes<STREAM>(pa + (a0 * (D / 2) + at + i * 2 * D));
+      kreg[4 + i] = load_codes<STREAM>(pb + (b0 * (D / 2) + at + i * 2 * D));
     }
     ksa = *reinterpret_cast<const int *>(pa + (ks_at + a0 * (D / 32)));
     ksb = *reinterpret_cast<const int *>(pb + (ks_at + b0 * (D / 32)));
@@ -295,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   auto load_v = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const p = part_of(d, g) + (w.v_off + slot_of(tile, g) * (D / 2) + col * 16);
 #pragma unroll
-    for (int m = 0; m < ND; ++m) vreg[m] = *reinterpret_cast<const int4v *>(p + m * 256);
+    for (int m = 0; m < ND; ++m) vreg[m] = load_codes<STREAM>(p + m * 256);
   };
 
   float m_run = -INFINITY, m_use = 0.0f, l_run = 0.0f;
@@ -883,35 +890,49 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
       make_uint2(eq_dev::pack_bf16(o.x * inv, o.y * inv), eq_dev::pack_bf16(o.z * inv, o.w * inv));
 }
 
-// How a call is launched.  Up to kFewCols columns of a key/value head and
-// sequence go to attn_kernel, more to prompt_kernel.  The token tiles are cut
-// into chunks so that the blocks fill the card about twice over, none shorter
-// than four tiles (attn_kernel: one for each wavefront) and, where there is less
-// than that to fill it with, none longer than 4096 tokens: a ragged batch's
-// longest sequence then spreads over the card too.
+// How a call is launched.
+//
+// Which kernel: prompt_kernel's tiles of 128 columns pay where they fill the card
+// by themselves, a block for each of 256 compute units, or where a long cache can
+// be cut into chunks; attn_kernel spreads fewer columns better.  Columns of a
+// key/value head, sequences x heads, cached tokens: us of attn_kernel / of
+// prompt_kernel
+//   64, 8 x 32, 1024: 26.8 / 27.7    128, 8 x 32, 1024: 46.0 / 31.2
+//   384, 8 x 8, 1024: 27.7 / 28.8    512, 8 x 8, 1024: 35.2 / 29.8
+//   1024, 1 x 8, 2048: 16.5 / 36.9   1024, 1 x 8, 8192: 68 / 58
+//   512, 1 x 8, 8192: 39.2 / 38.0    2048, 1 x 8, 32768: 418 / 301
+//
+// Chunks: the token tiles are cut so that the blocks fill the card about twice
+// over, none shorter than four tiles (attn_kernel: one for each wavefront) and,
+// where there is less than that to fill it with, none longer than 2048 tokens: a
+// ragged batch's longest sequence then spreads over the card too.  Up to 1536
+// tokens (attn_kernel) are one chunk: a further tile for a wavefront is 1.4 us,
+// the second launch 3.7.  prompt_kernel's partial sums are larger (4096 columns,
+// 1 x 8, 8192 tokens: 165 us in one chunk, 187 in two), so it has chunks only
+// where the columns do not fill the card.
 struct Plan {
   bool prompt;
   uint32_t cols, tile, q_tiles, chunks, chunk_tiles;
 };
 
-constexpr uint32_t kFewCols = 64;
-constexpr uint32_t kWholeTiles = 16;
+constexpr uint32_t kFewCols = 64, kFillBlocks = 256, kWholeTiles = 12, kLongTokens = 8192;
 
 Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_new,
                uint32_t max_len, uint32_t window) {
   Plan p;
   const uint64_t cols = uint64_t(max_new) * group;
-  p.prompt = cols > kFewCols;
+  const uint64_t prompts = uint64_t(n_seqs) * kv_heads * ((cols + kPromptCols - 1) / kPromptCols);
+  p.prompt = cols > kFewCols && (prompts >= kFillBlocks || max_len >= kLongTokens);
   p.cols = p.prompt ? kPromptCols : kCols;
   p.tile = p.prompt ? kPromptTile : kTile;
   p.q_tiles = uint32_t((cols + p.cols - 1) / p.cols);
   const uint64_t work = uint64_t(n_seqs) * kv_heads * p.q_tiles;
   const uint32_t tiles = (max_len + p.tile - 1) / p.tile;
-  const uint64_t want = std::max<uint64_t>(1, (512 + work - 1) / work);
+  const bool whole = p.prompt ? work >= kFillBlocks : tiles <= kWholeTiles;
+  const uint64_t want = whole ? 1 : std::max<uint64_t>(1, (512 + work - 1) / work);
   auto round4 = [](uint64_t v) { return uint32_t(std::max<uint64_t>((v + 3) / 4 * 4, 4)); };
   uint32_t ct = round4((tiles + want - 1) / want);
-  if (work < (p.prompt ? 512 : 2048)) ct = std::min(ct, 4096 / p.tile);
-  if (!p.prompt && tiles <= kWholeTiles) ct = round4(tiles);
+  if (!whole && work < 2048) ct = std::min(ct, 2048 / p.tile);
   p.chunks = std::max((tiles + ct - 1) / ct, 1u);
   // a window leaves fewer tiles (a query's window and the others' of its
   // sequence), in at most as many chunks: the workspace does not depend on it
@@ -937,8 +958,8 @@ size_t attn_bytes(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
 }
 
 template <int D>
-void launch_attn(const AttnArgs &a, const Plan &p, bool one_page, dim3 grid, dim3 join,
-                 hipStream_t stream) {
+void launch_attn(const AttnArgs &a, const Plan &p, bool one_page, bool stream_codes, dim3 grid,
+                 dim3 join, hipStream_t stream) {
   const dim3 block(256), join_block(2 * D);
   if (p.prompt) {
     hipLaunchKernelGGL(prompt_kernel<D>, grid, block, 0, stream, a);
@@ -946,8 +967,9 @@ void launch_attn(const AttnArgs &a, const Plan &p, bool one_page, dim3 grid, dim
       hipLaunchKernelGGL((join_kernel<D, kPromptCols, kPromptTile>), join, join_block, 0, stream, a);
     return;
   }
-  if (one_page) hipLaunchKernelGGL((attn_kernel<D, true>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((attn_kernel<D, false>), grid, block, 0, stream, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+  if (one_page) stream_codes ? go(attn_kernel<D, true, true>) : go(attn_kernel<D, true, false>);
+  else stream_codes ? go(attn_kernel<D, false, true>) : go(attn_kernel<D, false, false>);
   if (p.chunks > 1)
     hipLaunchKernelGGL((join_kernel<D, kCols, kTile>), join, join_block, 0, stream, a);
 }
@@ -991,7 +1013,15 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
   const dim3 grid(uint32_t(blocks), batch->n_seqs), join(uint32_t(joins), batch->n_seqs);
   const bool one_page = cache->page_tokens >= kTile;
-  if (cache->head_dim == 128) launch_attn<128>(a, p, one_page, grid, join, stream);
-  else launch_attn<64>(a, p, one_page, grid, join, stream);
+  // Codes that are read once in all, and more of them than the memory-side cache
+  // holds (256 MiB), pass the caches as streams: 284 000 tokens of 8 heads 74 ->
+  // 70 us.  Smaller caches stay in it between calls (16 MiB: 7.5 us, as streams
+  // 8.1), and query tiles share what the first of them has read.
+  const bool stream_codes =
+      p.q_tiles == 1 && uint64_t(batch->n_seqs) * batch->max_len * cache->kv_heads *
+                                (cache->head_dim + cache->head_dim / 32 + 1) >
+                            uint64_t(192) << 20;
+  if (cache->head_dim == 128) launch_attn<128>(a, p, one_page, stream_codes, grid, join, stream);
+  else launch_attn<64>(a, p, one_page, stream_codes, grid, join, stream);
   return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP;
 }

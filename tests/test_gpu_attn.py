@@ -101,15 +101,21 @@ CASES = [
     ([3], [2600], 4, 2, 128, 64, 2300),
     ([200], [1500], 2, 1, 128, 64, 0),
     ([300], [300], 3, 3, 64, 32, 0),
+    # many columns in all: 128 of them in a block
+    ([40, 33, 36, 0, 38], [140, 33, 200, 0, 71], 128, 64, 128, 32, 0),
+    ([66, 33, 70, 35], [66, 133, 90, 171], 128, 64, 64, 64, 50),
 ]
 
 
+# bound 8192: columns in blocks of 128 wherever there are more than 64 of a
+# sequence and head, and cached tokens in chunks
+@pytest.mark.parametrize("bound", [0, 8192])
 @pytest.mark.parametrize("news,lens,hq,hk,dim,page,window", CASES)
-def test_attention(eq, news, lens, hq, hk, dim, page, window):
-    say("attn", news, lens, hq, hk, dim, page, window)
+def test_attention(eq, news, lens, hq, hk, dim, page, window, bound):
+    say("attn", news, lens, hq, hk, dim, page, window, bound)
     r = np.random.default_rng(sum(lens) + hq)
     n_pages = sum(-(-t // page) for t in lens) + 1
-    b, starts, table = batch(eq, news, lens, page, n_pages, seed=5)
+    b, starts, table = batch(eq, news, lens, page, n_pages, seed=5, bound=bound)
     cache, k, v, _ = filled(eq, r, lens, page, hk, dim, n_pages, b, starts)
     q = dev(r.standard_normal((starts[-1], hq, dim)).astype(np.float32), torch.bfloat16) * 2
     out = torch.full((starts[-1], hq, dim), 7.0, dtype=torch.bfloat16, device="cuda")
@@ -124,30 +130,33 @@ def test_attention(eq, news, lens, hq, hk, dim, page, window):
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
 
 
-def test_rows_before_the_first_token_are_zero(eq):
+@pytest.mark.parametrize("hq,bound", [(2, 0), (32, 8192)])
+def test_rows_before_the_first_token_are_zero(eq, hq, bound):
     """More new rows than tokens: the rows that have no position see nothing."""
     r = np.random.default_rng(2)
-    b, starts, table = batch(eq, [5], [3], 32, 2)
+    b, starts, table = batch(eq, [5], [3], 32, 2, bound=bound)
     full, _, _ = batch(eq, [3], [3], 32, 2)
     cache, k, v, _ = filled(eq, r, [3], 32, 1, 64, 2, full, None)
-    q = dev(r.standard_normal((5, 2, 64)).astype(np.float32), torch.bfloat16)
-    out = torch.full((5, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
-    eq.eq_attn_kv4(cache, b, q, 0.125, out, eq.attn_workspace(cache, b, 2))
+    q = dev(r.standard_normal((5, hq, 64)).astype(np.float32), torch.bfloat16)
+    out = torch.full((5, hq, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    eq.eq_attn_kv4(cache, b, q, 0.125, out, eq.attn_workspace(cache, b, hq))
     o = out.double().cpu().numpy()
     assert (o[:2] == 0).all()
     check(o[2:], q.double().cpu().numpy()[2:], k, v, [3], [3], 0.125, 0)
 
 
-def test_absent_pages_are_absent_tokens(eq):
+@pytest.mark.parametrize("bound", [0, 8192])
+def test_absent_pages_are_absent_tokens(eq, bound):
     r = np.random.default_rng(4)
     lens, news, page, hk, dim = [300, 90], [2, 90], 32, 2, 128
-    b, starts, table = batch(eq, news, lens, page, 14)
+    b, starts, table = batch(eq, news, lens, page, 14, bound=bound)
     cache, k, v, _ = filled(eq, r, lens, page, hk, dim, 14, b, starts)
     gone = table.copy()
     gone[0, [0, 5]], gone[1, :2] = [-1, 14], [-3, 1 << 30]
     present = [np.ones(300, bool), np.ones(90, bool)]
     present[0][0:32] = present[0][160:192] = present[1][0:64] = False
-    b2 = eq.KvBatch(b.tensors[0], b.tensors[1], dev(gone), n_tokens=92, max_new=90, max_len=300)
+    b2 = eq.KvBatch(b.tensors[0], b.tensors[1], dev(gone), n_tokens=92, max_new=90,
+                    max_len=max(300, bound))
     q = dev(r.standard_normal((92, 4, dim)).astype(np.float32), torch.bfloat16)
     out = torch.full((92, 4, dim), 7.0, dtype=torch.bfloat16, device="cuda")
     eq.eq_attn_kv4(cache, b2, q, dim ** -0.5, out, eq.attn_workspace(cache, b2, 4))
@@ -156,13 +165,14 @@ def test_absent_pages_are_absent_tokens(eq):
     assert (o[2:66] == 0).all()  # rows that see absent pages alone
 
 
-@pytest.mark.parametrize("dim,new", [(64, 1), (128, 1), (128, 24), (64, 150)])
-def test_sharp_scores_and_values_of_unlike_size(eq, dim, new):
+@pytest.mark.parametrize("dim,new,bound", [(64, 1, 0), (128, 1, 0), (128, 24, 0), (128, 24, 8192),
+                                           (64, 150, 0), (64, 150, 8192)])
+def test_sharp_scores_and_values_of_unlike_size(eq, dim, new, bound):
     """Scores up to hundreds (P from 1 to an underflow), values that differ by
     2^40 between the tokens of a tile, zero queries, zero values."""
     r = np.random.default_rng(dim + new)
     lens, page = [290], 64
-    b, starts, _ = batch(eq, [new], lens, page, 5)
+    b, starts, _ = batch(eq, [new], lens, page, 5, bound=bound)
     cache, k, v, whole = filled(eq, r, lens, page, 1, dim, 5, b, starts)
     kd = dev(r.standard_normal((290, 1, dim)).astype(np.float32))
     vd = dev(r.standard_normal((290, 1, dim)).astype(np.float32))
@@ -180,12 +190,13 @@ def test_sharp_scores_and_values_of_unlike_size(eq, dim, new):
           vo.double().cpu().numpy(), [new], lens, dim ** -0.5, 0)
 
 
+@pytest.mark.parametrize("bound", [0, 8192])
 @pytest.mark.parametrize("dim,new,heads", [(128, 40, 2), (64, 40, 2), (128, 150, 4)])
-def test_nan_reaches_those_that_see_it(eq, dim, new, heads):
+def test_nan_reaches_those_that_see_it(eq, dim, new, heads, bound):
     r = np.random.default_rng(6)
     lens, page, news = [new + 160], 32, [new]
     t = lens[0]
-    b, starts, _ = batch(eq, news, lens, page, t // 32 + 1)
+    b, starts, _ = batch(eq, news, lens, page, t // 32 + 1, bound=bound)
     cache, _, _, whole = filled(eq, r, lens, page, 1, dim, t // 32 + 1, b, starts)
     for which in ("k", "v", "q"):
         kd, vd = torch.randn(2, t, 1, dim, device="cuda")

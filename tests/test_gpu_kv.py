@@ -35,11 +35,12 @@ def tables(rows, half, seed=0):
     return np.cos(a).astype(np.float32), np.sin(a).astype(np.float32)
 
 
-def batch(eq, news, lens, page, n_pages, seed=0, **over):
-    """A batch over a shuffled pool: (KvBatch, starts, page table)."""
+def batch(eq, news, lens, page, n_pages, seed=0, bound=0, **over):
+    """A batch over a shuffled pool: (KvBatch, starts, page table).  bound: the
+    most tokens that the page table has room for, where that is more."""
     r = np.random.default_rng(seed)
     starts = np.concatenate(([0], np.cumsum(news))).astype(np.int32)
-    width = max(1, max(-(-t // page) for t in lens))
+    width = max(1, -(-max(max(lens), bound) // page))
     free = r.permutation(n_pages).astype(np.int32)
     table = np.full((len(lens), width), -1, dtype=np.int32)
     at = 0
@@ -47,7 +48,7 @@ def batch(eq, news, lens, page, n_pages, seed=0, **over):
         n = -(-t // page)
         table[i, :n] = free[at:at + n]
         at += n
-    a = dict(n_tokens=int(starts[-1]), max_new=max(news), max_len=max(lens))
+    a = dict(n_tokens=int(starts[-1]), max_new=max(news), max_len=max(max(lens), bound))
     a.update(over)
     b = eq.KvBatch(dev(starts), dev(np.array(lens, dtype=np.int32)), dev(table), **a)
     return b, starts, table
