@@ -367,7 +367,7 @@ size_t eq_kv_page_bytes(uint32_t kv_heads, uint32_t head_dim, uint32_t page_toke
  * at their place in the sequence; the rotation is in fp32 (each product and
  * the sum rounded) and the result is rounded once, to its code.  Other tokens
  * of the pages keep their values.  Two sequences of one call may share pages,
- * but not 8 consecutive tokens that either appends to. */
+ * but not 8 aligned positions that either appends to. */
 int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, const void *k,
                  uint64_t k_stride, const void *v, uint64_t v_stride, uint32_t dtype,
                  const int32_t *positions, const eq_rope *rope, hipStream_t stream);

@@ -66,85 +66,100 @@ struct NormArgs {
   Rope rope;
   uint32_t tokens, q_heads, k_heads, dim;
   float eps;
+  bool wide_weights;  // 16-byte aligned
+  uint32_t parts;     // blocks of a token
 };
 
 // A head is held by L lanes (a power of two, dim/8 rounded up), 8 consecutive
-// channels a lane, so a wavefront normalises 64/L heads at once: the mean is
-// log2 L exchanges, a rotation by halves one more (channels c and c + half are
-// half/8 lanes apart, half being a multiple of 8), and every load and store
-// is 16 bytes a lane.  A lane has all of its inputs before its first store, and
-// a head is one wavefront's, so BF16 rows may be rewritten in place.
+// channels a lane: the mean is log2 L exchanges, a rotation by halves one more
+// (channels c and c + half are half/8 lanes apart, half being a multiple of 8),
+// and every load and store is 16 bytes a lane.  A block takes heads of one token,
+// 256/L side by side, so that they share what its position reads.  A lane has all
+// of a head before it stores any of it, and a head is one wavefront's, so BF16
+// rows may be rewritten in place.
+//
+// Bound by memory: 8192 tokens of 72 heads of 128, BF16: 306 MB in 61.7 us, 4.96
+// TB/s (a 1 GiB device copy: 5.07).  Heads in no order of tokens, each with its
+// own table rows, took 79 us; two or three heads in flight for a lane 65 and 70,
+// fewer wavefronts being resident then.
 template <typename T, int L, bool VEC>
 __global__ __launch_bounds__(256) void norm_rope_kernel(NormArgs a) {
+  constexpr uint32_t kSide = 256 / L;
   const uint32_t heads = a.q_heads + a.k_heads;
-  const uint64_t item = (uint64_t(blockIdx.x) * 256 + threadIdx.x) / L;
-  const uint32_t l = threadIdx.x % L, c0 = 8 * l;
-  const bool on = item < uint64_t(a.tokens) * heads && c0 < a.dim;
-  const uint32_t t = on ? uint32_t(item / heads) : 0, h = on ? uint32_t(item % heads) : 0;
-  const bool is_k = h >= a.q_heads;
-  const uint32_t hh = is_k ? h - a.q_heads : h;
-  const uint16_t *const weight = is_k ? a.k_weight : a.q_weight;
-  float x[8] = {};
-  if (on)
-    load_row<T, 8, VEC>(static_cast<const T *>(is_k ? a.k : a.q) +
-                            t * (is_k ? a.k_stride : a.q_stride) + uint64_t(hh) * a.dim + c0, x);
-  float ss = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-#pragma unroll
-  for (int d = 1; d < L; d *= 2) ss += __shfl_xor(ss, d);
-  if (weight && on) {
-    const float r = rsqrtf(ss / float(a.dim) + a.eps);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * r * bf16_to_f32(weight[c0 + i]);
-  }
-  const uint32_t half = a.rope.half;
-  if (half) {
-    const bool turned = on && c0 < 2 * half;
-    const uint64_t at = uint64_t(turned ? table_row(a.rope, a.positions[t]) : 0) * half;
+  const uint32_t t = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const uint32_t c0 = 8 * (threadIdx.x % L), half = a.rope.half;
+  const bool turned = c0 < 2 * half, upper = c0 >= half && !a.rope.pairs;
+  float cs[8] = {}, sn[8] = {};
+  if (turned) {
+    const uint64_t at = uint64_t(table_row(a.rope, a.positions[t])) * half;
     if (a.rope.pairs) {
+      load_row<float, 4, true>(a.rope.cos + at + c0 / 2, cs);
+      load_row<float, 4, true>(a.rope.sin + at + c0 / 2, sn);
+    } else {
+      load_row<float, 8, true>(a.rope.cos + at + (upper ? c0 - half : c0), cs);
+      load_row<float, 8, true>(a.rope.sin + at + (upper ? c0 - half : c0), sn);
+    }
+  }
+  for (uint32_t h0 = part * kSide; h0 < heads; h0 += a.parts * kSide) {
+    const uint32_t h = h0 + threadIdx.x / L;
+    const bool on = h < heads && c0 < a.dim, is_k = h >= a.q_heads;
+    const uint16_t *const weight = is_k ? a.k_weight : a.q_weight;
+    float x[8] = {};
+    if (on)
+      load_row<T, 8, VEC>(is_k ? static_cast<const T *>(a.k) + t * a.k_stride +
+                                     uint64_t(h - a.q_heads) * a.dim + c0
+                               : static_cast<const T *>(a.q) + t * a.q_stride + uint64_t(h) * a.dim + c0,
+                          x);
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
+#pragma unroll
+    for (int d = 1; d < L; d *= 2) ss += __shfl_xor(ss, d);
+    if (weight && on) {
+      const float r = rsqrtf(ss / float(a.dim) + a.eps);
+      float wt[8];
+      if (a.wide_weights) load_row<uint16_t, 8, true>(weight + c0, wt);
+      else load_row<uint16_t, 8, false>(weight + c0, wt);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = x[i] * r * wt[i];
+    }
+    if (half && a.rope.pairs) {
       if (turned) {
-        float c[4], s[4];
-        *reinterpret_cast<float4 *>(c) = *reinterpret_cast<const float4 *>(a.rope.cos + at + c0 / 2);
-        *reinterpret_cast<float4 *>(s) = *reinterpret_cast<const float4 *>(a.rope.sin + at + c0 / 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float u = x[2 * i], v = x[2 * i + 1];
-          x[2 * i] = u * c[i] - v * s[i];
-          x[2 * i + 1] = v * c[i] + u * s[i];
+          x[2 * i] = u * cs[i] - v * sn[i];
+          x[2 * i + 1] = v * cs[i] + u * sn[i];
         }
       }
-    } else {
-      const bool upper = c0 >= half;
+    } else if (half) {
       const uint32_t step = half / 8, lane = threadIdx.x & 63;
       const uint32_t other = turned ? (upper ? lane - step : lane + step) : lane;
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], int(other));
       if (turned) {
-        float c[8], s[8];
-        const uint64_t o = at + (upper ? c0 - half : c0);
-        load_row<float, 8, true>(a.rope.cos + o, c);
-        load_row<float, 8, true>(a.rope.sin + o, s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i] + (upper ? y[i] : -y[i]) * s[i];
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * cs[i] + (upper ? y[i] : -y[i]) * sn[i];
       }
     }
-  }
-  if (on) {
-    uint16_t *const out = (is_k ? a.k_out : a.q_out) +
-                          (uint64_t(t) * (is_k ? a.k_heads : a.q_heads) + hh) * a.dim + c0;
-    *reinterpret_cast<uint4 *>(out) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
-                                                 pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    if (on) {
+      uint16_t *const out = is_k ? a.k_out + (uint64_t(t) * a.k_heads + h - a.q_heads) * a.dim + c0
+                                 : a.q_out + (uint64_t(t) * a.q_heads + h) * a.dim + c0;
+      *reinterpret_cast<uint4 *>(out) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
+                                                   pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
   }
 }
 
+// Few tokens: a block for each 256/L heads, so that no head waits for another's;
+// many: one for a token.
 template <typename T, bool VEC>
-void launch_norm(const NormArgs &a, hipStream_t stream) {
-  const uint64_t items = uint64_t(a.tokens) * (a.q_heads + a.k_heads);
+void launch_norm(NormArgs a, hipStream_t stream) {
   auto go = [&](auto kernel, uint32_t lanes) {
-    hipLaunchKernelGGL(kernel, dim3(uint32_t((items * lanes + 255) / 256)), dim3(256), 0, stream,
-                       a);
+    const uint32_t per = 256 / lanes;
+    a.parts = a.tokens < 256 ? (a.q_heads + a.k_heads + per - 1) / per : 1;
+    hipLaunchKernelGGL(kernel, dim3(a.tokens * a.parts), dim3(256), 0, stream, a);
   };
   const uint32_t need = a.dim / 8;
   if (need <= 2) go(norm_rope_kernel<T, 2, VEC>, 2);
@@ -168,9 +183,14 @@ struct AppendArgs {
 // and this lane's N values; infinities and NaN sort above every number.
 template <int N, int G>
 __device__ inline uint32_t group_top(const float *x) {
-  uint32_t m = 0;
+  float top = 0.0f;  // (the maximum passes over NaN)
+  bool nan = false;
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+  for (int i = 0; i < N; i += 2) {
+    top = fmaxf(top, fmaxf(fabsf(x[i]), fabsf(x[i + 1])));
+    nan = nan || __builtin_isunordered(x[i], x[i + 1]);
+  }
+  uint32_t m = nan ? 0x7FC00000u : __float_as_uint(top);
 #pragma unroll
   for (int d = 1; d < G; d *= 2) m = max(m, uint32_t(__shfl_xor(int(m), d)));
   return m;
@@ -253,7 +273,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t grou
   constexpr int N = D / 8;           // channels a lane
   __shared__ __attribute__((aligned(16))) uint8_t lds[4][8][D / 2 + 4];
   const View &w = a.w;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
   const uint32_t s = blockIdx.y;
   const uint32_t item = blockIdx.x * 4 + wave;  // (group, head), heads within groups
   const Seq q = sequence(w, s);
@@ -262,37 +282,35 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t grou
   const int32_t end = min(q.base + q.count, int32_t(w.max_len));
   int32_t page = -1;
   if (item < groups * w.kv_heads && q.count > 0 && first < end)
-    page = eq_dev::uniform(page_of(w, s, first));
+    page = page_of(w, s, first);
   const uint32_t t = lane >> 3, sub = lane & 7, e0 = sub * N;
   const int32_t pos = first + int32_t(t);
   const bool on = page >= 0 && pos >= q.base && pos < end;
   const uint32_t slot = uint32_t(pos) & ((1u << w.page_shift) - 1);
   uint8_t *const part = w.pages + uint64_t(max(page, 0)) * w.page_bytes + uint64_t(h) * w.head_bytes;
   const uint64_t row = on ? uint64_t(q.row) + (pos - q.base) : 0;
-  float x[N] = {};
+  float x[N] = {}, v[N] = {};
   if (on) {
     const T *const kr = static_cast<const T *>(a.k) + row * a.k_stride + uint64_t(h) * D;
     load_row<T, N, VEC>(kr + e0, x);
+    load_row<T, N, VEC>(static_cast<const T *>(a.v) + row * a.v_stride + uint64_t(h) * D + e0, v);
     if (a.rope.half) rotate_key<T, N, VEC>(a.rope, kr, e0, a.positions ? a.positions[row] : pos, x);
   }
   constexpr int kPerBlock = 32 / N;  // lanes of a key group
   uint32_t b = scale_byte(group_top<N, kPerBlock>(x));
   if (on) {
     uint32_t *const kc = reinterpret_cast<uint32_t *>(part + slot * (D / 2) + e0 / 2);
-#pragma unroll
-    for (int i = 0; i < N / 8; ++i) kc[i] = codes8(x + 8 * i, b);
+    if constexpr (N == 16) *reinterpret_cast<uint2 *>(kc) = make_uint2(codes8(x, b), codes8(x + 8, b));
+    else *kc = codes8(x, b);
     if (sub % kPerBlock == 0)
       part[w.ks_off + slot / 16 * (D / 2) + (slot % 4 * (D / 32) + sub / kPerBlock) * 4 +
            slot % 16 / 4] = uint8_t(b);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = 0.0f;
-    load_row<T, N, VEC>(static_cast<const T *>(a.v) + row * a.v_stride + uint64_t(h) * D + e0, x);
   }
-  b = scale_byte(group_top<N, 8>(x));
+  b = scale_byte(group_top<N, 8>(v));
   if (on && sub == 0) part[w.vs_off + slot] = uint8_t(b);
 #pragma unroll
   for (int i = 0; i < N / 8; ++i)
-    *reinterpret_cast<uint32_t *>(&lds[wave][t][e0 / 2 + 4 * i]) = codes8(x + 8 * i, b);
+    *reinterpret_cast<uint32_t *>(&lds[wave][t][e0 / 2 + 4 * i]) = codes8(v + 8 * i, b);
   const uint64_t mask = __ballot(on);
   __syncthreads();
   if (page < 0 || lane >= D / 2) return;
@@ -325,60 +343,71 @@ __device__ inline uint32_t bf16_pair(uint32_t byte, uint32_t b) {
   return b == 255 ? 0x7FC07FC0u : v;
 }
 
-// The same 8 positions of a head for each wavefront as in append_kernel: keys
-// a lane's D/8 channels of one token, values two channels of eight tokens (a
-// dword each), which leave as whole rows.
+// A unit of 32 positions of a head for each wavefront, its loads in flight
+// together (8 positions, a quarter of the bytes for the same chain of loads, took
+// 47 us where this takes 42): of keys a lane has D/8 channels of four tokens, of
+// values two channels of all 32, which leave as whole rows.
 template <int D>
 __global__ __launch_bounds__(256) void read_kernel(View w, uint16_t *k, uint16_t *v,
-                                                   uint32_t groups) {
+                                                   uint32_t units) {
   constexpr int N = D / 8;
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
   const uint32_t s = blockIdx.y;
   const uint32_t item = blockIdx.x * 4 + wave;
-  if (item >= groups * w.kv_heads) return;
+  if (item >= units * w.kv_heads) return;
   const Seq q = sequence(w, s);
   const uint32_t h = item % w.kv_heads;
-  const int32_t first = (max(q.base, 0) & ~7) + 8 * int32_t(item / w.kv_heads);
+  const int32_t first = (max(q.base, 0) & ~31) + 32 * int32_t(item / w.kv_heads);
   const int32_t end = min(q.base + q.count, int32_t(w.max_len));
   if (q.count <= 0 || first >= end) return;
-  const int32_t page = eq_dev::uniform(page_of(w, s, first));
+  const int32_t page = page_of(w, s, first);
   if (page < 0) return;
   const uint32_t slot0 = uint32_t(first) & ((1u << w.page_shift) - 1);
   const uint8_t *const part = w.pages + uint64_t(page) * w.page_bytes + uint64_t(h) * w.head_bytes;
-  auto out_row = [&](int32_t pos) {
-    return ((uint64_t(q.row) + (pos - q.base)) * w.kv_heads + h) * D;
-  };
   const uint32_t t = lane >> 3, sub = lane & 7, e0 = sub * N;
-  const int32_t pos = first + int32_t(t);
-  uint2 vc = make_uint2(0, 0);
-  if (lane < D / 2) {
-    const uint32_t *const p = reinterpret_cast<const uint32_t *>(
-        part + w.v_off + (slot0 / 32 * D + 2 * lane) * 16 + slot0 % 32 / 2);
-    vc = make_uint2(p[0], p[4]);
+  uint4 vc[2], vs[2];
+  uint32_t kc[4][N / 8], kb[4];
+  // (what is read of tokens that are not asked for is in the unit all the same)
+  const uint32_t pair = min(lane, uint32_t(D / 2 - 1));
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    vc[i] = *reinterpret_cast<const uint4 *>(part + w.v_off + (slot0 / 32 * D + 2 * pair + i) * 16);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    vs[i] = *reinterpret_cast<const uint4 *>(part + w.vs_off + slot0 + 16 * i);
+#pragma unroll
+  for (uint32_t g = 0; g < 4; ++g) {
+    const uint32_t slot = slot0 + 8 * g + t;
+    const uint32_t *const p = reinterpret_cast<const uint32_t *>(part + slot * (D / 2) + e0 / 2);
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) kc[g][i] = p[i];
+    kb[g] = part[w.ks_off + slot / 16 * (D / 2) + (slot % 4 * (D / 32) + e0 / 32) * 4 + slot % 16 / 4];
   }
-  const uint2 vs = *reinterpret_cast<const uint2 *>(part + w.vs_off + slot0);
-  if (pos >= q.base && pos < end) {
-    const uint32_t slot = slot0 + t;
-    const uint32_t *const kc = reinterpret_cast<const uint32_t *>(part + slot * (D / 2) + e0 / 2);
-    const uint32_t b = part[w.ks_off + slot / 16 * (D / 2) + (slot % 4 * (D / 32) + e0 / 32) * 4 +
-                            slot % 16 / 4];
-    uint32_t *const out = reinterpret_cast<uint32_t *>(k + out_row(pos) + e0);
+  const uint64_t step = uint64_t(w.kv_heads) * D;  // elements between the rows of two tokens
+  const int64_t row0 = (int64_t(q.row) + (first - q.base)) * int64_t(step) + int64_t(h) * D;
+#pragma unroll
+  for (uint32_t g = 0; g < 4; ++g) {
+    const int32_t pos = first + int32_t(8 * g + t);
+    if (pos < q.base || pos >= end) continue;
+    uint16_t *const out = k + row0 + int64_t(8 * g + t) * int64_t(step) + e0;
 #pragma unroll
     for (int i = 0; i < N / 8; ++i) {
-      const uint32_t c = kc[i];
-      *reinterpret_cast<uint4 *>(out + 4 * i) =
+      const uint32_t c = kc[g][i], b = kb[g];
+      *reinterpret_cast<uint4 *>(out + 8 * i) =
           make_uint4(bf16_pair(c & 255, b), bf16_pair(c >> 8 & 255, b), bf16_pair(c >> 16 & 255, b),
                      bf16_pair(c >> 24, b));
     }
   }
   if (lane >= D / 2) return;
+  const uint32_t lo[4] = {vc[0].x, vc[0].y, vc[0].z, vc[0].w};
+  const uint32_t hi[4] = {vc[1].x, vc[1].y, vc[1].z, vc[1].w};
+  const uint32_t sc[8] = {vs[0].x, vs[0].y, vs[0].z, vs[0].w, vs[1].x, vs[1].y, vs[1].z, vs[1].w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int32_t p = first + i;
-    if (p < q.base || p >= end) continue;
-    const uint32_t byte = (vc.x >> (4 * i) & 15) | (vc.y >> (4 * i) & 15) << 4;
-    const uint32_t b = (i < 4 ? vs.x : vs.y) >> (8 * (i & 3)) & 255;
-    *reinterpret_cast<uint32_t *>(v + out_row(p) + 2 * lane) = bf16_pair(byte, b);
+  for (int i = 0; i < 32; ++i) {
+    if (first + i < q.base || first + i >= end) continue;
+    const uint32_t byte = (lo[i / 8] >> (4 * (i % 8)) & 15) | (hi[i / 8] >> (4 * (i % 8)) & 15) << 4;
+    *reinterpret_cast<uint32_t *>(v + row0 + int64_t(i) * int64_t(step) + 2 * lane) =
+        bf16_pair(byte, sc[i / 4] >> (8 * (i % 4)) & 255);
   }
 }
 
@@ -401,8 +430,8 @@ bool aligned16(const void *p, uint64_t stride_bytes) {
 
 int done() { return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP; }
 
-// Groups of 8 aligned positions that `max_new` consecutive ones can touch.
-uint32_t position_groups(uint32_t max_new) { return (max_new + 6) / 8 + 1; }
+// Aligned runs of `run` positions that `max_new` consecutive ones can touch.
+uint32_t position_runs(uint32_t max_new, uint32_t run) { return (max_new + run - 2) / run + 1; }
 
 }  // namespace
 
@@ -422,10 +451,12 @@ extern "C" int eq_qk_norm_rope(const void *q, uint64_t q_stride, uint32_t q_head
                    (tokens > 1 && k_stride < uint64_t(k_heads) * head_dim))))
     return EQ_EINVAL;
   if (tokens == 0 || heads == 0) return EQ_OK;
-  if (uint64_t(tokens) * heads > (uint64_t(1) << 33)) return EQ_EINVAL;  // grid below 2^31
+  if (tokens > 1u << 30) return EQ_EINVAL;  // grid below 2^31
   const uint64_t item = dtype == EQ_F32 ? 4 : 2;
   NormArgs a{q, k, q_stride, k_stride, q_weight, k_weight, q_out, k_out, positions,
-             device_rope(rope), tokens, q_heads, k_heads, head_dim, eps};
+             device_rope(rope), tokens, q_heads, k_heads, head_dim, eps,
+             ((reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) & 15) == 0,
+             0};
   const bool vec = (!q_heads || aligned16(q, q_stride * item)) &&
                    (!k_heads || aligned16(k, k_stride * item));
   if (dtype == EQ_F32) vec ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
@@ -449,7 +480,7 @@ extern "C" int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, 
   AppendArgs a{view(cache, batch), k, v, k_stride, v_stride, positions, device_rope(rope)};
   const uint64_t item = dtype == EQ_F32 ? 4 : 2;
   const bool vec = aligned16(k, k_stride * item) && aligned16(v, v_stride * item);
-  const uint32_t groups = position_groups(batch->max_new);
+  const uint32_t groups = position_runs(batch->max_new, 8);
   const uint64_t blocks = (uint64_t(groups) * cache->kv_heads + 3) / 4;
   if (blocks > 0x7FFFFFFFu) return EQ_EINVAL;
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
@@ -472,15 +503,15 @@ extern "C" int eq_kv_read(const eq_kv_cache *cache, const eq_kv_batch *batch, ui
   if (batch->n_seqs == 0 || batch->max_new == 0 || batch->max_len == 0) return EQ_OK;
   if (!k || !v || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15))
     return EQ_EINVAL;
-  const uint32_t groups = position_groups(batch->max_new);
-  const uint64_t blocks = (uint64_t(groups) * cache->kv_heads + 3) / 4;
+  const uint32_t units = position_runs(batch->max_new, 32);
+  const uint64_t blocks = (uint64_t(units) * cache->kv_heads + 3) / 4;
   if (blocks > 0x7FFFFFFFu) return EQ_EINVAL;
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
   if (cache->head_dim == 128)
     hipLaunchKernelGGL((read_kernel<128>), grid, dim3(256), 0, stream, view(cache, batch), k, v,
-                       groups);
+                       units);
   else
     hipLaunchKernelGGL((read_kernel<64>), grid, dim3(256), 0, stream, view(cache, batch), k, v,
-                       groups);
+                       units);
   return done();
 }
