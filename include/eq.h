@@ -362,15 +362,16 @@ int eq_qk_norm_rope(const void *q, uint64_t q_stride, uint32_t q_heads, const ui
 size_t eq_kv_page_bytes(uint32_t kv_heads, uint32_t head_dim, uint32_t page_tokens);
 
 /* Append a batch's rows to the cache: k and v are n_tokens rows of kv_heads x
- * head_dim elements of `dtype`, k_stride and v_stride elements apart.  With
- * rope, keys are rotated on the way, at positions[row] or, when that is NULL,
- * at their place in the sequence; the rotation is in fp32 (each product and
- * the sum rounded) and the result is rounded once, to its code.  Other tokens
+ * head_dim elements of `k_dtype` and `v_dtype`, k_stride and v_stride elements
+ * apart.  With rope, keys are rotated on the way, at positions[row] or, when that
+ * is NULL, at their place in the sequence; the rotation is in fp32 (each product
+ * and the sum rounded) and the result is rounded once, to its code.  Other tokens
  * of the pages keep their values.  Two sequences of one call may share pages,
  * but not 8 aligned positions that either appends to. */
 int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, const void *k,
-                 uint64_t k_stride, const void *v, uint64_t v_stride, uint32_t dtype,
-                 const int32_t *positions, const eq_rope *rope, hipStream_t stream);
+                 uint64_t k_stride, uint32_t k_dtype, const void *v, uint64_t v_stride,
+                 uint32_t v_dtype, const int32_t *positions, const eq_rope *rope,
+                 hipStream_t stream);
 
 /* The values that the cache holds for a batch's rows, as BF16 (exact), to k
  * and v: contiguous [n_tokens][kv_heads][head_dim], 16-byte aligned.  With

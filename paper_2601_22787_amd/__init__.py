@@ -108,8 +108,8 @@ SIGNATURES = {
                                        ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32,
                                        ctypes.c_float, _vp, _vp, _vp]),
     "eq_kv_page_bytes": (ctypes.c_size_t, [ctypes.c_uint32, ctypes.c_uint32, ctypes.c_uint32]),
-    "eq_kv_append": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, _vp, ctypes.c_uint64,
-                                    ctypes.c_uint32, _vp, _vp, _vp]),
+    "eq_kv_append": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, ctypes.c_uint32, _vp,
+                                    ctypes.c_uint64, ctypes.c_uint32, _vp, _vp, _vp]),
     "eq_kv_read": (ctypes.c_int, [_vp, _vp, _vp, _vp, _vp]),
     "eq_attn_kv4_workspace_bytes": (ctypes.c_size_t, [_vp, _vp, ctypes.c_uint32]),
     "eq_attn_kv4": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_float,
@@ -537,14 +537,12 @@ def eq_kv_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
 
 
 def eq_kv_append(cache, batch, k, v, *, rope=None, positions=None, stream=None) -> None:
-    """Append k and v [n_tokens, kv_heads, head_dim] (fp32 or BF16), the keys
-    rotated on the way when rope is given: at `positions`, or at the tokens'
-    places in their sequences."""
-    pk, sk, kind = _cache_rows(k, cache, batch, "k")
+    """Append k and v [n_tokens, kv_heads, head_dim] (fp32 or BF16 each), the
+    keys rotated on the way when rope is given: at `positions`, or at the
+    tokens' places in their sequences."""
+    pk, sk, kind_k = _cache_rows(k, cache, batch, "k")
     pv, sv, kind_v = _cache_rows(v, cache, batch, "v")
-    if kind != kind_v:
-        raise ValueError("k and v differ in type")
-    rc = lib().eq_kv_append(cache.ptr, batch.ptr, pk, sk, pv, sv, kind,
+    rc = lib().eq_kv_append(cache.ptr, batch.ptr, pk, sk, kind_k, pv, sv, kind_v,
                             _positions(positions, batch.n_tokens),
                             None if rope is None else rope.ptr, _stream(stream))
     if rc:

@@ -268,7 +268,7 @@ __device__ inline void rotate_key(const Rope &r, const T *row, uint32_t e0, int3
 // two exchanges, its value scale three.  Value codes go through LDS, a row of
 // D/2 bytes a token, and come back as a column of bytes, two channels of eight
 // tokens, that is repacked into the two channels' dwords.
-template <typename T, int D, bool VEC>
+template <typename TK, typename TV, int D, bool VEC>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t groups) {
   constexpr int N = D / 8;           // channels a lane
   __shared__ __attribute__((aligned(16))) uint8_t lds[4][8][D / 2 + 4];
@@ -291,10 +291,10 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t grou
   const uint64_t row = on ? uint64_t(q.row) + (pos - q.base) : 0;
   float x[N] = {}, v[N] = {};
   if (on) {
-    const T *const kr = static_cast<const T *>(a.k) + row * a.k_stride + uint64_t(h) * D;
-    load_row<T, N, VEC>(kr + e0, x);
-    load_row<T, N, VEC>(static_cast<const T *>(a.v) + row * a.v_stride + uint64_t(h) * D + e0, v);
-    if (a.rope.half) rotate_key<T, N, VEC>(a.rope, kr, e0, a.positions ? a.positions[row] : pos, x);
+    const TK *const kr = static_cast<const TK *>(a.k) + row * a.k_stride + uint64_t(h) * D;
+    load_row<TK, N, VEC>(kr + e0, x);
+    load_row<TV, N, VEC>(static_cast<const TV *>(a.v) + row * a.v_stride + uint64_t(h) * D + e0, v);
+    if (a.rope.half) rotate_key<TK, N, VEC>(a.rope, kr, e0, a.positions ? a.positions[row] : pos, x);
   }
   constexpr int kPerBlock = 32 / N;  // lanes of a key group
   uint32_t b = scale_byte(group_top<N, kPerBlock>(x));
@@ -469,31 +469,42 @@ extern "C" size_t eq_kv_page_bytes(uint32_t kv_heads, uint32_t head_dim, uint32_
   return size_t(head_bytes(head_dim, page_tokens)) * kv_heads;
 }
 
+namespace {
+
+template <typename TK, typename TV>
+void launch_append(const AppendArgs &a, uint32_t head_dim, bool vec, uint32_t groups, dim3 grid,
+                   hipStream_t stream) {
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, groups); };
+  if (head_dim == 128) vec ? go(append_kernel<TK, TV, 128, true>) : go(append_kernel<TK, TV, 128, false>);
+  else vec ? go(append_kernel<TK, TV, 64, true>) : go(append_kernel<TK, TV, 64, false>);
+}
+
+}  // namespace
+
 extern "C" int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, const void *k,
-                            uint64_t k_stride, const void *v, uint64_t v_stride, uint32_t dtype,
-                            const int32_t *positions, const eq_rope *rope, hipStream_t stream) {
-  if (!batch_ok(cache, batch) || dtype > EQ_BF16 || !rope_ok(rope, cache->head_dim))
+                            uint64_t k_stride, uint32_t k_dtype, const void *v, uint64_t v_stride,
+                            uint32_t v_dtype, const int32_t *positions, const eq_rope *rope,
+                            hipStream_t stream) {
+  if (!batch_ok(cache, batch) || k_dtype > EQ_BF16 || v_dtype > EQ_BF16 ||
+      !rope_ok(rope, cache->head_dim))
     return EQ_EINVAL;
   if (batch->n_seqs == 0 || batch->max_new == 0 || batch->max_len == 0) return EQ_OK;
   const uint64_t width = uint64_t(cache->kv_heads) * cache->head_dim;
   if (!k || !v || (batch->n_tokens > 1 && (k_stride < width || v_stride < width))) return EQ_EINVAL;
   AppendArgs a{view(cache, batch), k, v, k_stride, v_stride, positions, device_rope(rope)};
-  const uint64_t item = dtype == EQ_F32 ? 4 : 2;
-  const bool vec = aligned16(k, k_stride * item) && aligned16(v, v_stride * item);
+  const bool vec = aligned16(k, k_stride * (k_dtype == EQ_F32 ? 4 : 2)) &&
+                   aligned16(v, v_stride * (v_dtype == EQ_F32 ? 4 : 2));
   const uint32_t groups = position_runs(batch->max_new, 8);
   const uint64_t blocks = (uint64_t(groups) * cache->kv_heads + 3) / 4;
   if (blocks > 0x7FFFFFFFu) return EQ_EINVAL;
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
-  auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, groups);
-  };
-  if (cache->head_dim == 128) {
-    if (dtype == EQ_F32) vec ? go(append_kernel<float, 128, true>) : go(append_kernel<float, 128, false>);
-    else vec ? go(append_kernel<uint16_t, 128, true>) : go(append_kernel<uint16_t, 128, false>);
-  } else {
-    if (dtype == EQ_F32) vec ? go(append_kernel<float, 64, true>) : go(append_kernel<float, 64, false>);
-    else vec ? go(append_kernel<uint16_t, 64, true>) : go(append_kernel<uint16_t, 64, false>);
-  }
+  const uint32_t d = cache->head_dim;
+  if (k_dtype == EQ_F32)
+    v_dtype == EQ_F32 ? launch_append<float, float>(a, d, vec, groups, grid, stream)
+                      : launch_append<float, uint16_t>(a, d, vec, groups, grid, stream);
+  else
+    v_dtype == EQ_F32 ? launch_append<uint16_t, float>(a, d, vec, groups, grid, stream)
+                      : launch_append<uint16_t, uint16_t>(a, d, vec, groups, grid, stream);
   return done();
 }
 

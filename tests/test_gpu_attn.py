@@ -263,7 +263,7 @@ def test_graph_of_a_generation_step(eq, max_len):
 
     def step(c, o, ws):
         eq.eq_qk_norm_rope(xq, xk, o[0], o[1], q_weight=w, k_weight=w, rope=rope, positions=pos)
-        eq.eq_kv_append(c, b, o[1], xv.to(torch.bfloat16))
+        eq.eq_kv_append(c, b, o[1], xv)
         eq.eq_attn_kv4(c, b, o[0], dim ** -0.5, o[2], ws)
 
     ca, oa = state()

@@ -132,10 +132,14 @@ APPEND = [
     ([23, 1, 8], [150, 129, 8], 1, 128, 128, 16, False, "f32", "odd"),
     ([40], [90], 2, 64, 4096, 48, True, "bf16", "odd"),
     ([33, 5], [70, 6], 2, 64, 32, 16, False, "f32", "fused"),
+    ([3, 20], [30, 20], 2, 128, 64, 128, False, "bf16 f32", "plain"),
+    ([9], [19], 1, 64, 32, 32, True, "f32 bf16", "plain"),
 ]
 
 
 def _rows(r, tokens, heads, dim, dtype, layout):
+    if " " in dtype:  # keys and values of two types
+        return tuple(_rows(r, tokens, heads, dim, d, layout)[i] for i, d in enumerate(dtype.split()))
     kind = torch.float32 if dtype == "f32" else torch.bfloat16
     x = r.standard_normal((tokens, 2 * heads * dim + 8)) * np.exp(r.standard_normal((tokens, 1)) * 2)
     x = dev(x.astype(np.float32), kind)

@@ -35,8 +35,8 @@ def ref(x):
     return None if x is None else ctypes.addressof(x)
 
 
-def append(c, b, k=P, ks=256, v=P, vs=256, kind=0, r=None):
-    return eq.lib().eq_kv_append(ref(c), ref(b), k, ks, v, vs, kind, None, ref(r), None)
+def append(c, b, k=P, ks=256, kk=0, v=P, vs=256, kv=1, r=None):
+    return eq.lib().eq_kv_append(ref(c), ref(b), k, ks, kk, v, vs, kv, None, ref(r), None)
 
 
 def read(c, b, k=P, v=P):
@@ -89,7 +89,7 @@ def test_nothing_to_do(call):
 
 
 def test_append_refusals():
-    for a in (dict(k=None), dict(v=None), dict(ks=255), dict(vs=255), dict(kind=2)):
+    for a in (dict(k=None), dict(v=None), dict(ks=255), dict(vs=255), dict(kk=2), dict(kv=2)):
         assert append(cache(), batch(), **a) == eq.EQ_EINVAL, a
     for a in (dict(cos=None), dict(sin=P + 8), dict(rows=0), dict(dims=0), dict(dims=24),
               dict(dims=144)):
