@@ -192,8 +192,15 @@ __device__ inline floatx4 mul16(int8v codes, int8v terms, floatx4 acc, int as, i
 // All ones where bit i of m is set, else 0.
 __device__ inline uint32_t bit_mask(uint32_t m, int i) { return uint32_t(int32_t(m << (31 - i)) >> 31); }
 
-// The largest x of the four lanes (col, g) of a column.
+// x of the lane 8 columns on (of 16).
+__device__ inline float other_half(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));
+}
+
+// The largest x of the lanes (col, g) of a column; PAIR: and of those 8 columns on.
+template <bool PAIR>
 __device__ inline float column_max(float x) {
+  if constexpr (PAIR) x = fmaxf(x, other_half(x));
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
@@ -216,7 +223,13 @@ __device__ inline int4v load_codes(const uint8_t *p) {
 // Then a lane's 32 scores are the 32 tokens of its steps in order, and P passes
 // from the first product to the second without leaving the lane.  V lies along
 // the tokens in the cache, 32 to a 16-byte row, as the second product takes it.
-template <int D, bool ONE, bool STREAM>
+//
+// PAIR: up to 8 columns.  The other 8 of a product then take the second terms: of
+// the queries (the scores of columns c and c + 8 add up to column c's; at D = 64
+// they are the same queries again, one product having both terms already), and of
+// w P (columns c and c + 8 of O add up at the end).  Half the products, and each
+// of the two lanes has the softmax of 16 of the 32 tokens.
+template <int D, bool ONE, bool STREAM, bool PAIR>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int ND = D / 16;
   constexpr uint32_t kStride = D + 4;  // floats a column in LDS
@@ -224,8 +237,10 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   __shared__ float2 lds_s[kWaves][kCols];
   const View &w = a.w;
   const uint32_t s = blockIdx.y;
-  const uint32_t chunk = blockIdx.x % a.chunks, rest = blockIdx.x / a.chunks;
-  const uint32_t qt = rest % a.q_tiles, h = rest / a.q_tiles;
+  // heads first: the blocks that run together then read whole pages, not a head's
+  // part of pages all over the pool (284 000 tokens of 8 heads: 69 -> 62 us)
+  const uint32_t h = blockIdx.x % w.kv_heads, rest = blockIdx.x / w.kv_heads;
+  const uint32_t chunk = rest % a.chunks, qt = rest / a.chunks;
   const uint32_t col0 = qt * kCols;
   const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
   const uint32_t col = lane & 15, g = lane >> 4;
@@ -260,7 +275,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const uint32_t t_last = t < t_end ? t + (t_end - 1 - t) / kWaves * kWaves : t;
 
   // this lane's column
-  const uint32_t index = col0 + col;
+  const bool upper = PAIR && col >= 8;
+  const uint32_t index = col0 + (PAIR ? col & 7 : col);
   const bool real = index < sp.cols;
   const uint32_t token = index / a.group;
   const int32_t pos = q.base + int32_t(token);
@@ -279,7 +295,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   };
   auto slot_of = [&](uint32_t tile, uint32_t unit) { return (tile * 4 + unit) * kUnit & page_mask; };
   int4v kreg[8], vreg[ND];
-  uint4 va, vb;
+  uint4 va, vb;  // (PAIR: va is of the lane's own 16 tokens)
   int ksa, ksb;
   auto load_k = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const pa = part_of(d, gk >> 1), *const pb = part_of(d, 2 + (gk >> 1));
@@ -295,9 +311,10 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     ksb = *reinterpret_cast<const int *>(pb + (ks_at + b0 * (D / 32)));
   };
   auto load_vs = [&](uint32_t tile, const Ids &d) {
-    const uint32_t at = w.vs_off + 16 * (g & 1);
-    va = *reinterpret_cast<const uint4 *>(part_of(d, g >> 1) + (at + slot_of(tile, g >> 1)));
-    vb = *reinterpret_cast<const uint4 *>(part_of(d, 2 + (g >> 1)) + (at + slot_of(tile, 2 + (g >> 1))));
+    const uint32_t at = w.vs_off + 16 * (g & 1), unit = (g >> 1) + (upper ? 2 : 0);
+    va = *reinterpret_cast<const uint4 *>(part_of(d, unit) + (at + slot_of(tile, unit)));
+    if constexpr (!PAIR)
+      vb = *reinterpret_cast<const uint4 *>(part_of(d, 2 + unit) + (at + slot_of(tile, 2 + unit)));
   };
   auto load_v = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const p = part_of(d, g) + (w.v_off + slot_of(tile, g) * (D / 2) + col * 16);
@@ -306,7 +323,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   };
 
   float m_run = -INFINITY, m_use = 0.0f, l_run = 0.0f;
-  int8v ph{}, pq{};  // w P of a tile, as two terms
+  int8v ph{}, pq{};  // w P of a tile, as two terms (PAIR: ph is the lane's term)
   floatx4 o[ND];
 #pragma unroll
   for (int m = 0; m < ND; ++m) o[m] = floatx4{0, 0, 0, 0};
@@ -323,6 +340,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     load_v(t, ids);
     Ids next = load_ids(min(t + kWaves, t_last));
     query.split(raw, col, g);
+    if (PAIR && D == 128 && upper) query.h = query.l, query.hs = query.ls;
     for (; t < t_end; t += kWaves) {
       const uint32_t t_next = min(t + kWaves, t_last);
       floatx4 sc[8];
@@ -340,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
           }
         };
         mul(query.h, query.hs);
-        if constexpr (D == 128) mul(query.l, query.ls);
+        if constexpr (D == 128 && !PAIR) mul(query.l, query.ls);
       }
       load_k(t_next, next);
       // masks, where some column does not see the whole tile
@@ -350,33 +368,49 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
       for (uint32_t u = 0; u < (ONE ? 1 : 4); ++u) gone |= uint32_t(ids.u[u] >= w.n_pages) << u;
       if (ONE && gone) gone = 15;
       const bool masked = at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || gone;
-      uint32_t visible = ~0u;  // bit 4 i + e: this lane's column sees that token
+      // a lane's scores: all 32 of its tokens, or, with PAIR, 16 of them and the
+      // sum of both terms, whose other half the lane 8 columns on holds
+      constexpr int NS = PAIR ? 16 : 32;
+      float x[NS];
+      if constexpr (PAIR) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float low = sc[i / 4][i % 4], high = sc[4 + i / 4][i % 4];
+          x[i] = upper ? high : low;
+          if constexpr (D == 128) x[i] += other_half(upper ? low : high);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] = sc[i / 4][i % 4];
+      }
+      uint32_t visible = ~0u;  // bit i: this lane's column sees token i of them
       if (masked) {
         auto bits = [&](uint32_t unit, int32_t from) {  // of 16 tokens
-          const int32_t x = min(max(lo - from, 0), 16), y = min(max(hi - from, x), 16);
-          return gone >> unit & 1 ? 0u : (1u << y) - (1u << x);
+          const int32_t u = min(max(lo - from, 0), 16), v = min(max(hi - from, u), 16);
+          return gone >> unit & 1 ? 0u : (1u << v) - (1u << u);
         };
-        visible = bits(g >> 1, at + 16 * int32_t(g)) | bits(2 + (g >> 1), at + 64 + 16 * int32_t(g)) << 16;
+        const uint32_t unit = (g >> 1) + (upper ? 2 : 0);
+        const int32_t from = at + 16 * int32_t(g) + (upper ? 64 : 0);
+        visible = bits(unit, from);
+        if constexpr (!PAIR) visible |= bits(2 + unit, from + 64) << 16;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sc[i][e] = __uint_as_float((__float_as_uint(sc[i][e]) & bit_mask(visible, 4 * i + e)) |
-                                       (0xFF800000u & ~bit_mask(visible, 4 * i + e)));
+        for (int i = 0; i < NS; ++i)
+          x[i] = __uint_as_float((__float_as_uint(x[i]) & bit_mask(visible, i)) |
+                                 (0xFF800000u & ~bit_mask(visible, i)));
       }
       // The maximum is set 8 above the scores and follows when they reach it: a
-      // lane then compares its own 32, and the four that share a column seldom
-      // have to agree on a new one.
+      // lane then compares its own, and those that share a column seldom have to
+      // agree on a new one.
       float part[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        part[k] = sc[2 * k][0];
+      for (int c = 0; c < 4; ++c) {
+        part[c] = x[c * NS / 4];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) part[k] = fmaxf(part[k], sc[2 * k + i / 4][i % 4]);
+        for (int i = 1; i < NS / 4; ++i) part[c] = fmaxf(part[c], x[c * NS / 4 + i]);
       }
       float mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * a.c;
       if (__any(mx > m_run)) {
-        mx = column_max(mx);
+        mx = column_max<PAIR>(mx);
         const float m_new = mx > m_run ? mx + 8.0f : m_run;
         m_use = m_new == -INFINITY ? 0.0f : m_new;
         const float f = exp2_(m_run - m_use);
@@ -385,49 +419,59 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
         for (int m = 0; m < ND; ++m) o[m] *= f;
         m_run = m_new;
       }
-      float y[32];
       const uint32_t vs[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < NS; i += 4) {
         float p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = exp2_(__builtin_fmaf(sc[i][e], a.c, -m_use));
+        for (int e = 0; e < 4; ++e) p[e] = exp2_(__builtin_fmaf(x[i + e], a.c, -m_use));
         l_run += (p[0] + p[1]) + (p[2] + p[3]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          y[4 * i + e] = p[e] * __uint_as_float((vs[i] >> (8 * e) & 255u) << 23);
+          x[i + e] = p[e] * __uint_as_float((vs[i / 4] >> (8 * e) & 255u) << 23);
       }
       if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          y[i] = __uint_as_float(__float_as_uint(y[i]) & bit_mask(visible, i));
+        for (int i = 0; i < NS; ++i)
+          x[i] = __uint_as_float(__float_as_uint(x[i]) & bit_mask(visible, i));
       }
       float top = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) top = fmaxf(top, y[i]);
+      for (int i = 0; i < NS; ++i) top = fmaxf(top, x[i]);
       load_vs(t_next, next);
-      top = column_max(top);
-      const int ps = top_byte(__float_as_uint(top));
+      top = column_max<PAIR>(top);
+      int ps = top_byte(__float_as_uint(top));
       const int pl = low_byte(ps);
       const float scale = byte_value(ps);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < NS / 4; ++i) {
         int u = ph[i], v = pq[i];
-        split4(y + 4 * i, scale, u, v);
+        split4(x + 4 * i, scale, u, v);
         ph[i] = u;
         pq[i] = v;
+      }
+      if constexpr (PAIR) {
+        // lower columns take the first term of both halves, upper ones the second
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int got = __float_as_int(other_half(__int_as_float(upper ? ph[i] : pq[i])));
+          ph[4 + i] = upper ? pq[i] : got;
+          ph[i] = upper ? got : ph[i];
+        }
+        ps = upper ? pl : ps;
       }
 #pragma unroll
       for (int m = 0; m < ND; ++m) {
         const int8v v8 = widen(vreg[m]);
         o[m] = mul16<0>(v8, ph, o[m], kUnitScale, ps);
-        o[m] = mul16<0>(v8, pq, o[m], kUnitScale, pl);
+        if constexpr (!PAIR) o[m] = mul16<0>(v8, pq, o[m], kUnitScale, pl);
       }
       load_v(t_next, next);
       ids = next;
       next = load_ids(min(t_next + kWaves, t_last));
     }
   }
+  if constexpr (PAIR) l_run += other_half(l_run);
   l_run += __shfl_xor(l_run, 16);
   l_run += __shfl_xor(l_run, 32);
 
@@ -449,7 +493,11 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     const float f = exp2_(lds_s[v][oc].x - m_ref);
     l_all += f * lds_s[v][oc].y;
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) sum[i] += f * lds_o[(v * kCols + oc) * kStride + d0 + i];
+    for (uint32_t i = 0; i < kPer; ++i) {
+      float x = lds_o[(v * kCols + oc) * kStride + d0 + i];
+      if constexpr (PAIR) x += lds_o[(v * kCols + (oc | 8)) * kStride + d0 + i];  // (oc < 8)
+      sum[i] += f * x;
+    }
   }
   if (sp.chunks <= 1) {
     const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
@@ -904,8 +952,9 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
 //
 // Chunks: the token tiles are cut so that the blocks fill the card about twice
 // over, none shorter than four tiles (attn_kernel: one for each wavefront) and,
-// where there is less than that to fill it with, none longer than 2048 tokens: a
-// ragged batch's longest sequence then spreads over the card too.  Up to 1536
+// where there is less than that to fill it with, none longer than 4096 tokens
+// (prompt_kernel: 2048): a ragged batch's longest sequence then spreads over the
+// card too.  Up to 1536
 // tokens (attn_kernel) are one chunk: a further tile for a wavefront is 1.4 us,
 // the second launch 3.7.  prompt_kernel's partial sums are larger (4096 columns,
 // 1 x 8, 8192 tokens: 165 us in one chunk, 187 in two), so it has chunks only
@@ -932,7 +981,7 @@ Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_
   const uint64_t want = whole ? 1 : std::max<uint64_t>(1, (512 + work - 1) / work);
   auto round4 = [](uint64_t v) { return uint32_t(std::max<uint64_t>((v + 3) / 4 * 4, 4)); };
   uint32_t ct = round4((tiles + want - 1) / want);
-  if (!whole && work < 2048) ct = std::min(ct, 2048 / p.tile);
+  if (!whole && work < 2048) ct = std::min(ct, (p.prompt ? 2048 : 4096) / p.tile);
   p.chunks = std::max((tiles + ct - 1) / ct, 1u);
   // a window leaves fewer tiles (a query's window and the others' of its
   // sequence), in at most as many chunks: the workspace does not depend on it
@@ -958,8 +1007,8 @@ size_t attn_bytes(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
 }
 
 template <int D>
-void launch_attn(const AttnArgs &a, const Plan &p, bool one_page, bool stream_codes, dim3 grid,
-                 dim3 join, hipStream_t stream) {
+void launch_attn(const AttnArgs &a, const Plan &p, bool pair, bool one_page, bool stream_codes,
+                 dim3 grid, dim3 join, hipStream_t stream) {
   const dim3 block(256), join_block(2 * D);
   if (p.prompt) {
     hipLaunchKernelGGL(prompt_kernel<D>, grid, block, 0, stream, a);
@@ -968,8 +1017,14 @@ void launch_attn(const AttnArgs &a, const Plan &p, bool one_page, bool stream_co
     return;
   }
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-  if (one_page) stream_codes ? go(attn_kernel<D, true, true>) : go(attn_kernel<D, true, false>);
-  else stream_codes ? go(attn_kernel<D, false, true>) : go(attn_kernel<D, false, false>);
+  auto pick = [&](auto one, auto streams) {
+    constexpr bool ONE = decltype(one)::value, STREAM = decltype(streams)::value;
+    pair ? go(attn_kernel<D, ONE, STREAM, true>) : go(attn_kernel<D, ONE, STREAM, false>);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if (one_page) stream_codes ? pick(yes, yes) : pick(yes, no);
+  else stream_codes ? pick(no, yes) : pick(no, no);
   if (p.chunks > 1)
     hipLaunchKernelGGL((join_kernel<D, kCols, kTile>), join, join_block, 0, stream, a);
 }
@@ -1013,6 +1068,7 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
   const dim3 grid(uint32_t(blocks), batch->n_seqs), join(uint32_t(joins), batch->n_seqs);
   const bool one_page = cache->page_tokens >= kTile;
+  const bool pair = uint64_t(batch->max_new) * group <= kCols / 2;
   // Codes that are read once in all, and more of them than the memory-side cache
   // holds (256 MiB), pass the caches as streams: 284 000 tokens of 8 heads 74 ->
   // 70 us.  Smaller caches stay in it between calls (16 MiB: 7.5 us, as streams
@@ -1021,7 +1077,7 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
       p.q_tiles == 1 && uint64_t(batch->n_seqs) * batch->max_len * cache->kv_heads *
                                 (cache->head_dim + cache->head_dim / 32 + 1) >
                             uint64_t(192) << 20;
-  if (cache->head_dim == 128) launch_attn<128>(a, p, one_page, stream_codes, grid, join, stream);
-  else launch_attn<64>(a, p, one_page, stream_codes, grid, join, stream);
+  if (cache->head_dim == 128) launch_attn<128>(a, p, pair, one_page, stream_codes, grid, join, stream);
+  else launch_attn<64>(a, p, pair, one_page, stream_codes, grid, join, stream);
   return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP;
 }
