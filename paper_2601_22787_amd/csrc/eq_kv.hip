@@ -15,7 +15,6 @@ using namespace eq_kv;
 using eq_dev::bf16_to_f32;
 using eq_dev::pack_bf16;
 
-typedef short short2v __attribute__((ext_vector_type(2)));
 
 struct Rope {
   const float *cos, *sin;
