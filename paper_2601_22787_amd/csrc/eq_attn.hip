@@ -9,8 +9,8 @@
 // cache, so neither keys nor values are ever decoded.  The other operand has to
 // be 8 bits wide: q and w P enter as the sum of two E4M3 numbers, x = h + l with
 // h = e4m3(x) and l = e4m3(x - h), 4 significant bits each.  That holds all of a
-// BF16 query, and w P to 8 significant bits, with a relative error below 2^-8 in
-// each term and no bias.
+// BF16 query that is at least 2^-14 of the largest of its 32 channels, and w P to 8
+// significant bits; what is smaller is held to 2^-21 of the largest.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -30,7 +30,6 @@ typedef short short2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 // Few query columns (attn_kernel): tokens a wavefront takes at a time, and the
@@ -228,7 +227,15 @@ __device__ inline int4v load_codes(const uint8_t *p) {
 // the queries (the scores of columns c and c + 8 add up to column c's; at D = 64
 // they are the same queries again, one product having both terms already), and of
 // w P (columns c and c + 8 of O add up at the end).  Half the products, and each
-// of the two lanes has the softmax of 16 of the 32 tokens.
+// of the two lanes has the softmax of 16 of the 32 tokens (284 000 tokens: 64.2 ->
+// 61.9 us; 512 tokens 5.75 -> 5.6).
+//
+// Long caches are bound by memory: one token of 14 sequences with 284 000 cached
+// ones, 64 query heads on 8, 303 MB in 62 us, 4.9 TB/s (a 1 GiB device copy:
+// 5.07); 3 wavefronts a SIMD by force spilled and took 82 us.  Short caches are
+// bound by the chain of one tile (page number, codes, two products with the
+// softmax between): 512 tokens of 32 heads 5.6 us, 8 x 4096 tokens 13.3 with the
+// join.
 template <int D, bool ONE, bool STREAM, bool PAIR>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int ND = D / 16;
@@ -579,6 +586,13 @@ struct PromptQuery {
 // The maximum is set 8 above the scores, and follows when they reach it: P stays
 // at most 1, and O is rescaled a few times in all, not whenever one of 32 columns
 // finds a larger score.
+//
+// 2048 new tokens behind 2048, 64 heads of 128 on 8: 206 GFLOP in 195 to 202 us,
+// 1.02 to 1.06 PFLOP/s (a large BF16 matrix product: 1.19); matrix units 44% and
+// vector units 46 to 53% busy, 7 wavefronts a compute unit.  Slower: both terms
+// of w P as E4M3 (278: registers spill), 8 wavefronts in two halves that take
+// turns (202), value codes brought to BF16 by each wavefront (201 against 197), 3
+// wavefronts a SIMD with the queries in LDS (272).
 template <int D>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   constexpr int ND = D / 32, KK = D / 64;
@@ -876,7 +890,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 
 // Joins the chunks of one query head at one new token, a block each: every
 // wavefront takes all chunks' maxima and sums, a lane each, and 8 groups of
-// threads the chunks' O in turn, added up through LDS.
+// threads the chunks' O in turn, added up through LDS.  Bound by its own latency:
+// 3.7 us, whatever the number of chunks up to 64.
 template <int D, uint32_t COLS, uint32_t TILE>
 __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   constexpr uint32_t kLanes = D / 4, kSub = 8;
@@ -1075,6 +1090,8 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
   if (need)
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
   const dim3 grid(uint32_t(blocks), batch->n_seqs), join(uint32_t(joins), batch->n_seqs);
+  // a tile in one page has one page number to read and take addresses from (284 000
+  // tokens: 61.9 us, as four 62.8)
   const bool one_page = cache->page_tokens >= kTile;
   const bool pair = uint64_t(batch->max_new) * group <= kCols / 2;
   // Codes that are read once in all, and more of them than the memory-side cache
