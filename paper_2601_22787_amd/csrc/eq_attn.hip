@@ -587,8 +587,8 @@ struct PromptQuery {
 // at most 1, and O is rescaled a few times in all, not whenever one of 32 columns
 // finds a larger score.
 //
-// 2048 new tokens behind 2048, 64 heads of 128 on 8: 206 GFLOP in 195 to 202 us,
-// 1.02 to 1.06 PFLOP/s (a large BF16 matrix product: 1.19); matrix units 44% and
+// 2048 new tokens behind 2048, 64 heads of 128 on 8: 206 GFLOP in 195 to 204 us,
+// 1.01 to 1.06 PFLOP/s (a large BF16 matrix product: 1.19); matrix units 44% and
 // vector units 46 to 53% busy, 7 wavefronts a compute unit.  Slower: both terms
 // of w P as E4M3 (278: registers spill), 8 wavefronts in two halves that take
 // turns (202), value codes brought to BF16 by each wavefront (201 against 197), 3

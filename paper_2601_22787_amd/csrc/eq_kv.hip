@@ -283,11 +283,12 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t grou
   const uint32_t item = blockIdx.x * 4 + wave;  // (group, head), heads within groups
   const Seq q = sequence(w, s);
   const uint32_t h = item % w.kv_heads;
-  const int32_t first = (max(q.base, 0) & ~7) + 8 * int32_t(item / w.kv_heads);
-  const int32_t end = min(q.base + q.count, int32_t(w.max_len));
-  int32_t page = -1;
-  if (item < groups * w.kv_heads && q.count > 0 && first < end)
-    page = page_of(w, s, first);
+  const int32_t start = max(q.base, 0), end = min(q.base + q.count, int32_t(w.max_len));
+  int32_t first = 0, page = -1;
+  if (item < groups * w.kv_heads && q.count > 0 && start < end) {
+    first = (start & ~7) + 8 * int32_t(item / w.kv_heads);  // (below 2^31: both are at most 2^30)
+    if (first < end) page = page_of(w, s, first);
+  }
   const uint32_t t = lane >> 3, sub = lane & 7, e0 = sub * N;
   const int32_t pos = first + int32_t(t);
   const bool on = page >= 0 && pos >= q.base && pos < end;
@@ -366,9 +367,10 @@ __global__ __launch_bounds__(256) void read_kernel(View w, uint16_t *k, uint16_t
   if (item >= units * w.kv_heads) return;
   const Seq q = sequence(w, s);
   const uint32_t h = item % w.kv_heads;
-  const int32_t first = (max(q.base, 0) & ~31) + 32 * int32_t(item / w.kv_heads);
-  const int32_t end = min(q.base + q.count, int32_t(w.max_len));
-  if (q.count <= 0 || first >= end) return;
+  const int32_t start = max(q.base, 0), end = min(q.base + q.count, int32_t(w.max_len));
+  if (q.count <= 0 || start >= end) return;
+  const int32_t first = (start & ~31) + 32 * int32_t(item / w.kv_heads);
+  if (first >= end) return;
   const int32_t page = page_of(w, s, first);
   if (page < 0) return;
   const uint32_t slot0 = uint32_t(first) & ((1u << w.page_shift) - 1);
@@ -505,7 +507,7 @@ extern "C" int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, 
                    aligned16(v, v_stride * (v_dtype == EQ_F32 ? 4 : 2));
   const uint32_t groups = position_runs(batch->max_new, 8);
   const uint64_t blocks = (uint64_t(groups) * cache->kv_heads + 3) / 4;
-  if (blocks > 0x7FFFFFFFu) return EQ_EINVAL;
+  if (blocks > 0x3FFFFFFFu) return EQ_EINVAL;  // (four wavefronts each: counted in 32 bits)
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
   const uint32_t d = cache->head_dim;
   if (k_dtype == EQ_F32)
@@ -525,7 +527,7 @@ extern "C" int eq_kv_read(const eq_kv_cache *cache, const eq_kv_batch *batch, ui
     return EQ_EINVAL;
   const uint32_t units = position_runs(batch->max_new, 32);
   const uint64_t blocks = (uint64_t(units) * cache->kv_heads + 3) / 4;
-  if (blocks > 0x7FFFFFFFu) return EQ_EINVAL;
+  if (blocks > 0x3FFFFFFFu) return EQ_EINVAL;  // (four wavefronts each: counted in 32 bits)
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
   if (cache->head_dim == 128)
     hipLaunchKernelGGL((read_kernel<128>), grid, dim3(256), 0, stream, view(cache, batch), k, v,

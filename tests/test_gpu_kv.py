@@ -271,6 +271,24 @@ def test_rows_and_pages_outside_the_bounds_are_skipped(eq):
         assert (o[:, ~left.cuda()] != 7.0).any(), over
 
 
+@pytest.mark.parametrize("length", [97, 2**30 + 5, 2**31 - 1])
+def test_rows_behind_the_longest_length_are_left_out(eq, length):
+    """One row a sequence, at the end of a length above the host's bound: the
+    cache and the outputs stay as they are."""
+    dim, page, heads = 64, 32, 2
+    base = np.random.default_rng(2).integers(0, 256, (3, kv_ref.page_bytes(heads, dim, page)),
+                                             dtype=np.uint8)
+    cache = eq.KvCache(dev(base), page_tokens=page, kv_heads=heads, head_dim=dim)
+    b = eq.KvBatch(dev(np.array([0, 1, 2], np.int32)), dev(np.array([length] * 2, np.int32)),
+                   dev(np.array([[0, 1, 2]] * 2, np.int32)), n_tokens=64, max_new=64, max_len=96)
+    k, v = torch.randn(2, 64, heads, dim, device="cuda")
+    eq.eq_kv_append(cache, b, k, v)
+    o = torch.full((2, 64, heads, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    eq.eq_kv_read(cache, b, o[0], o[1])
+    assert np.array_equal(cache.pages.cpu().numpy(), base)
+    assert (o == 7.0).all()
+
+
 def test_pool_beyond_32_bits(eq):
     """The last page of a pool of more than 4 GiB."""
     dim, page, heads = 128, 128, 8
