@@ -454,14 +454,15 @@ extern "C" int eq_qk_norm_rope(const void *q, uint64_t q_stride, uint32_t q_head
                                hipStream_t stream) {
   const uint64_t heads = uint64_t(q_heads) + k_heads;
   if (dtype > EQ_BF16 || head_dim == 0 || head_dim % 16 || head_dim > 256 || q_heads > 4096 ||
-      k_heads > 4096 || !rope_ok(rope, head_dim) || (rope && !positions) || !(eps >= 0.0f))
+      k_heads > 4096 || !rope_ok(rope, head_dim) || !(eps >= 0.0f))
     return EQ_EINVAL;
+  if (tokens == 0 || heads == 0) return EQ_OK;  // (a tensor of no tokens has no address)
+  if (rope && !positions) return EQ_EINVAL;
   if ((q_heads && (!q || !q_out || (reinterpret_cast<uintptr_t>(q_out) & 15) ||
                    (tokens > 1 && q_stride < uint64_t(q_heads) * head_dim))) ||
       (k_heads && (!k || !k_out || (reinterpret_cast<uintptr_t>(k_out) & 15) ||
                    (tokens > 1 && k_stride < uint64_t(k_heads) * head_dim))))
     return EQ_EINVAL;
-  if (tokens == 0 || heads == 0) return EQ_OK;
   if (tokens > 1u << 30) return EQ_EINVAL;  // grid below 2^31
   const uint64_t item = dtype == EQ_F32 ? 4 : 2;
   NormArgs a{q, k, q_stride, k_stride, q_weight, k_weight, q_out, k_out, positions,
