@@ -5,6 +5,8 @@
 // for prompts and the launch for single tokens.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "eq.h"
 #include "eq_device.h"
 #include "eq_kv.h"
@@ -151,13 +153,29 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormArgs a) {
 }
 
 // Few tokens: a block for each 256/L heads, so that no head waits for another's;
-// many: one for a token.
+// many: one for a token.  A launch has fewer than 2^32 threads along x, so more
+// tokens than kMostTokens are several launches.
+constexpr uint32_t kMostTokens = 1u << 23;
+
 template <typename T, bool VEC>
-void launch_norm(NormArgs a, hipStream_t stream) {
+void launch_norm(const NormArgs &a, hipStream_t stream) {
   auto go = [&](auto kernel, uint32_t lanes) {
     const uint32_t per = 256 / lanes;
-    a.parts = a.tokens < 256 ? (a.q_heads + a.k_heads + per - 1) / per : 1;
-    hipLaunchKernelGGL(kernel, dim3(a.tokens * a.parts), dim3(256), 0, stream, a);
+    for (uint64_t t = 0; t < a.tokens; t += kMostTokens) {
+      NormArgs b = a;
+      b.tokens = uint32_t(std::min<uint64_t>(a.tokens - t, kMostTokens));
+      b.parts = b.tokens < 256 ? (a.q_heads + a.k_heads + per - 1) / per : 1;
+      if (a.q_heads) {
+        b.q = static_cast<const T *>(a.q) + t * a.q_stride;
+        b.q_out = a.q_out + t * a.q_heads * a.dim;
+      }
+      if (a.k_heads) {
+        b.k = static_cast<const T *>(a.k) + t * a.k_stride;
+        b.k_out = a.k_out + t * a.k_heads * a.dim;
+      }
+      if (a.positions) b.positions = a.positions + t;
+      hipLaunchKernelGGL(kernel, dim3(b.tokens * b.parts), dim3(256), 0, stream, b);
+    }
   };
   const uint32_t need = a.dim / 8;
   if (need <= 2) go(norm_rope_kernel<T, 2, VEC>, 2);
@@ -463,7 +481,6 @@ extern "C" int eq_qk_norm_rope(const void *q, uint64_t q_stride, uint32_t q_head
       (k_heads && (!k || !k_out || (reinterpret_cast<uintptr_t>(k_out) & 15) ||
                    (tokens > 1 && k_stride < uint64_t(k_heads) * head_dim))))
     return EQ_EINVAL;
-  if (tokens > 1u << 30) return EQ_EINVAL;  // grid below 2^31
   const uint64_t item = dtype == EQ_F32 ? 4 : 2;
   NormArgs a{q, k, q_stride, k_stride, q_weight, k_weight, q_out, k_out, positions,
              device_rope(rope), tokens, q_heads, k_heads, head_dim, eps,
