@@ -322,13 +322,15 @@ typedef struct eq_kv_cache {
  * the launch depends on is in the host fields, which bound them.  Rows,
  * positions and pages outside the bounds (a page number below 0 marks a page
  * that is not there) are skipped: append and read leave out such tokens,
- * attention takes them for absent. */
+ * attention takes them for absent.  Bounds beyond one launch are refused: max_new
+ * kv_heads from about 2^29 (append) and 2^31 (read), max_new q_heads from 2^31
+ * (attention). */
 typedef struct eq_kv_batch {
   const int32_t *seq_start;  /* device: n_seqs + 1, ascending from >= 0            */
   const int32_t *kv_len;     /* device: n_seqs                                     */
   const int32_t *page_table; /* device: n_seqs x max_pages                         */
   uint32_t n_seqs;           /* at most 65535                                      */
-  uint32_t max_pages;
+  uint32_t max_pages;        /* >= 1                                               */
   uint32_t n_tokens;         /* rows of the dense arrays                           */
   uint32_t max_new;          /* bound of a sequence's rows                         */
   uint32_t max_len;          /* bound of kv_len (at most max_pages page_tokens)    */

@@ -1056,12 +1056,20 @@ bool heads_ok(const eq_kv_cache *c, uint32_t q_heads) {
   return q_heads >= 1 && q_heads % c->kv_heads == 0 && q_heads <= 65535;
 }
 
+// The columns of all heads are counted in 32 bits, and one launch takes them.  (A
+// window leaves fewer chunks, and chunks are joined where there are few columns.)
+bool size_ok(const eq_kv_cache *c, const eq_kv_batch *b, uint32_t q_heads) {
+  if (uint64_t(b->max_new) * q_heads > 0x7FFFFFFFu) return false;
+  const Plan p = plan_attn(b->n_seqs, c->kv_heads, q_heads / c->kv_heads, b->max_new, b->max_len, 0);
+  return uint64_t(c->kv_heads) * p.q_tiles * p.chunks <= kMaxBlocks;
+}
+
 }  // namespace
 
 extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
                                               uint32_t q_heads) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || batch->n_seqs == 0 ||
-      batch->max_new == 0)
+      batch->max_new == 0 || !size_ok(cache, batch, q_heads))
     return 0;
   return attn_bytes(plan_attn(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads,
                               batch->max_new, batch->max_len, 0),
@@ -1078,18 +1086,17 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
       q_stride % 8 || (batch->n_tokens > 1 && q_stride < uint64_t(q_heads) * cache->head_dim))
     return EQ_EINVAL;
   const uint32_t group = q_heads / cache->kv_heads;
+  if (!size_ok(cache, batch, q_heads)) return EQ_EINVAL;
   const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len,
                            window);
   const size_t need = attn_bytes(p, cache, batch);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return EQ_EINVAL;
-  const uint64_t blocks = uint64_t(cache->kv_heads) * p.q_tiles * p.chunks;
-  const uint64_t joins = uint64_t(batch->max_new) * q_heads;
-  if (blocks > 0x7FFFFFFFu || joins > 0x7FFFFFFFu) return EQ_EINVAL;
   AttnArgs a{view(cache, batch), q, q_stride, out, static_cast<float *>(ws), nullptr, group, window,
              p.q_tiles, p.chunks, p.chunk_tiles, scale * 1.44269504088896340736f};
   if (need)
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
-  const dim3 grid(uint32_t(blocks), batch->n_seqs), join(uint32_t(joins), batch->n_seqs);
+  const dim3 grid(cache->kv_heads * p.q_tiles * p.chunks, batch->n_seqs);
+  const dim3 join(batch->max_new * q_heads, batch->n_seqs);
   // a tile in one page has one page number to read and take addresses from (284 000
   // tokens: 61.9 us, as four 62.8)
   const bool one_page = cache->page_tokens >= kTile;

@@ -10,6 +10,8 @@
 namespace eq_kv {
 
 constexpr uint32_t kUnit = 32;  // tokens that share a block of value codes
+// A launch has fewer than 2^32 threads along x: the most blocks of 256.
+constexpr uint32_t kMaxBlocks = (1u << 24) - 1;
 
 // Offsets within a head's part of a page, and the batch, by value for kernels.
 struct View {

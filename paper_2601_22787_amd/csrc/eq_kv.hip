@@ -525,7 +525,7 @@ extern "C" int eq_kv_append(const eq_kv_cache *cache, const eq_kv_batch *batch, 
                    aligned16(v, v_stride * (v_dtype == EQ_F32 ? 4 : 2));
   const uint32_t groups = position_runs(batch->max_new, 8);
   const uint64_t blocks = (uint64_t(groups) * cache->kv_heads + 3) / 4;
-  if (blocks > 0x3FFFFFFFu) return EQ_EINVAL;  // (four wavefronts each: counted in 32 bits)
+  if (blocks > kMaxBlocks) return EQ_EINVAL;
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
   const uint32_t d = cache->head_dim;
   if (k_dtype == EQ_F32)
@@ -545,7 +545,7 @@ extern "C" int eq_kv_read(const eq_kv_cache *cache, const eq_kv_batch *batch, ui
     return EQ_EINVAL;
   const uint32_t units = position_runs(batch->max_new, 32);
   const uint64_t blocks = (uint64_t(units) * cache->kv_heads + 3) / 4;
-  if (blocks > 0x3FFFFFFFu) return EQ_EINVAL;  // (four wavefronts each: counted in 32 bits)
+  if (blocks > kMaxBlocks) return EQ_EINVAL;
   const dim3 grid(uint32_t(blocks), batch->n_seqs);
   if (cache->head_dim == 128)
     hipLaunchKernelGGL((read_kernel<128>), grid, dim3(256), 0, stream, view(cache, batch), k, v,

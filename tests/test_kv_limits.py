@@ -22,3 +22,24 @@ def test_norm_of_no_tokens(rope):
     # what is no size of a head stays refused
     assert eq.lib().eq_qk_norm_rope(None, 8, 64, None, None, None, 8, 8, None, None, 0, 0, 72, 1e-5,
                                     None, None, None) == eq.EQ_EINVAL
+
+
+def _bounds(heads, max_new):
+    c = eq.eq_kv_cache(P, 3, 64, heads, 128)
+    b = eq.eq_kv_batch(P, P, P, 1, 3, max_new, max_new, 100)
+    return c, b, heads * 128
+
+
+def test_bounds_beyond_one_launch_are_refused():
+    """2^32 threads along x and more: refused by the call, not by the launch."""
+    lib, at = eq.lib(), ctypes.addressof
+    for heads, max_new in ((8, 1 << 26), (1024, 1 << 19)):
+        c, b, width = _bounds(heads, max_new)
+        assert lib.eq_kv_append(at(c), at(b), P, width, 0, P, width, 0, None, None, None) == eq.EQ_EINVAL
+    c, b, width = _bounds(1024, 1 << 21)
+    assert lib.eq_kv_read(at(c), at(b), P, P, None) == eq.EQ_EINVAL
+    for heads, q_heads, max_new in ((1024, 1024, (1 << 21) - 1), (8, 64, 1 << 25), (1, 65535, 1 << 20)):
+        c, b, _ = _bounds(heads, max_new)
+        assert lib.eq_attn_kv4_workspace_bytes(at(c), at(b), q_heads) == 0
+        assert lib.eq_attn_kv4(at(c), at(b), P, q_heads * 128, q_heads, 1.0, 0, P, P, 1 << 60,
+                               None) == eq.EQ_EINVAL
