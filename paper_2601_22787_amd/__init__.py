@@ -434,8 +434,8 @@ class KvBatch:
             raise ValueError("seq_start has n + 1 entries, kv_len n, page_table n rows")
         if not kv_len.device == seq_start.device == page_table.device:
             raise ValueError("the batch's tensors are on several devices")
-        if min(n_tokens, max_new, max_len) < 0:
-            raise ValueError("negative bound")
+        if min(n_tokens, max_new, max_len) < 0 or max(n_tokens, max_new, max_len) >> 32:
+            raise ValueError("a bound below 0 or beyond 32 bits")
         self.tensors = (seq_start, kv_len, page_table)
         self.device = kv_len.device
         self.raw = eq_kv_batch(_dptr(seq_start, torch.int32), _dptr(kv_len, torch.int32),
@@ -509,6 +509,8 @@ def eq_qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: fl
     k may be None) and its rotation, to BF16: q_out, k_out contiguous."""
     shape = q.shape
     tokens, heads, dim = shape
+    if tokens >> 32:
+        raise ValueError("more than 2^32 - 1 tokens")
     pq, sq, kind = _head_rows(q, shape, "q")
     pqo = _bf16(q_out, tokens * heads * dim, "q_out")
     pk = pko = None
@@ -533,6 +535,8 @@ def eq_qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: fl
 
 
 def eq_kv_page_bytes(kv_heads: int, head_dim: int, page_tokens: int) -> int:
+    if (kv_heads | head_dim | page_tokens) >> 32:  # (ctypes would cut them; below 0 too)
+        return 0
     return lib().eq_kv_page_bytes(kv_heads, head_dim, page_tokens)
 
 
@@ -560,6 +564,8 @@ def eq_kv_read(cache, batch, k, v, stream=None) -> None:
 
 
 def eq_attn_kv4_workspace_bytes(cache, batch, q_heads: int) -> int:
+    if q_heads >> 32:
+        return 0
     return lib().eq_attn_kv4_workspace_bytes(cache.ptr, batch.ptr, q_heads)
 
 
@@ -575,6 +581,8 @@ def eq_attn_kv4(cache, batch, q, scale: float, out, ws=None, *, window: int = 0,
     """Causal attention of q [n_tokens, q_heads, head_dim] (BF16) over the
     cache to out (BF16, contiguous); with window, over the last `window`
     positions only."""
+    if window >> 32:  # (below 0 too)
+        raise ValueError(f"window {window}: expected 0 (none) to 2^32 - 1")
     shape = q.shape
     n, heads, dim = shape
     pq, sq, kind = _head_rows(q, shape, "q")

@@ -43,3 +43,43 @@ def test_bounds_beyond_one_launch_are_refused():
         assert lib.eq_attn_kv4_workspace_bytes(at(c), at(b), q_heads) == 0
         assert lib.eq_attn_kv4(at(c), at(b), P, q_heads * 128, q_heads, 1.0, 0, P, P, 1 << 60,
                                None) == eq.EQ_EINVAL
+
+
+@pytest.mark.parametrize("window", [-1, -(1 << 31), 1 << 32, (1 << 32) + 5])
+def test_windows_that_are_not_32_bits_are_refused(window):
+    torch = pytest.importorskip("torch")
+    q = torch.zeros(1, 1, 64)
+    with pytest.raises(ValueError, match="window"):
+        eq.eq_attn_kv4(None, None, q, 1.0, q, window=window)
+
+
+@pytest.mark.parametrize("over", [dict(n_tokens=(1 << 32) + 4), dict(max_new=1 << 32),
+                                  dict(max_len=(1 << 33) + 64), dict(max_len=-1)])
+def test_batch_bounds_that_are_not_32_bits_are_refused(over):
+    torch = pytest.importorskip("torch")
+    i = torch.zeros(3, dtype=torch.int32)
+    a = dict(n_tokens=4, max_new=2, max_len=64)
+    a.update(over)
+    with pytest.raises(ValueError, match="32 bits"):
+        eq.KvBatch(i, i[:2], i[:2].view(2, 1), **a)
+
+
+def test_sizes_that_are_not_32_bits_have_no_page_or_workspace():
+    for a in ((8 + (1 << 32), 128, 64), (8, 128 + (1 << 32), 64), (8, 128, 64 - (1 << 32))):
+        assert eq.eq_kv_page_bytes(*a) == 0, a
+
+    class Handle:
+        def __init__(self, raw):
+            self.raw, self.ptr = raw, ctypes.addressof(raw)
+
+    c = Handle(eq.eq_kv_cache(P, 3, 4096, 2, 128))
+    b = Handle(eq.eq_kv_batch(P, P, P, 2, 3, 4, 2, 12000))
+    assert eq.eq_attn_kv4_workspace_bytes(c, b, 4) > 0
+    assert eq.eq_attn_kv4_workspace_bytes(c, b, 4 + (1 << 32)) == 0
+
+
+def test_norm_of_more_tokens_than_32_bits_is_refused():
+    torch = pytest.importorskip("torch")
+    q = torch.zeros(1, 1, 16).expand((1 << 32) + 1, 1, 16)
+    with pytest.raises(ValueError, match="tokens"):
+        eq.eq_qk_norm_rope(q, None, q, None)
