@@ -386,8 +386,10 @@ class Rope:
         import torch
         if cos.dim() != 2 or cos.shape != sin.shape:
             raise ValueError("cos and sin are two [rows, dims / 2] tables")
+        if cos.device != sin.device:
+            raise ValueError("cos and sin are on two devices")
         self.tables = (cos, sin)
-        self.device = cos.device
+        self.device, self.index = cos.device, cos.get_device()
         self.raw = eq_rope(_dptr(cos, torch.float32), _dptr(sin, torch.float32), cos.shape[0],
                            2 * cos.shape[1], int(bool(pairs)))
         self.ptr = ctypes.addressof(self.raw)
@@ -407,7 +409,7 @@ class KvCache:
         if pages.numel() == 0 or pages.numel() % nbytes:
             raise ValueError(f"pages holds {pages.numel()} bytes, not a multiple of {nbytes}")
         self.pages, self.page_bytes = pages, nbytes
-        self.device = pages.device
+        self.device, self.index = pages.device, pages.get_device()
         self.raw = eq_kv_cache(ptr, pages.numel() // nbytes, page_tokens, kv_heads, head_dim)
         self.ptr = ctypes.addressof(self.raw)
         self.kv_heads, self.head_dim = kv_heads, head_dim
@@ -437,7 +439,7 @@ class KvBatch:
         if min(n_tokens, max_new, max_len) < 0 or max(n_tokens, max_new, max_len) >> 32:
             raise ValueError("a bound below 0 or beyond 32 bits")
         self.tensors = (seq_start, kv_len, page_table)
-        self.device = kv_len.device
+        self.device, self.index = kv_len.device, kv_len.get_device()
         self.raw = eq_kv_batch(_dptr(seq_start, torch.int32), _dptr(kv_len, torch.int32),
                                _dptr(page_table, torch.int32), n, page_table.shape[1], n_tokens,
                                max_new, max_len)
@@ -446,60 +448,84 @@ class KvBatch:
 
 
 _KINDS = {}  # torch dtype -> EQ_F32 or EQ_BF16, filled by the first call
-_BF16 = _I32 = None
+_BF16 = _I32 = _current = _raw_stream = None
 
 
 def _kinds():
-    global _BF16, _I32
+    global _BF16, _I32, _current, _raw_stream
     import torch
     _BF16, _I32 = torch.bfloat16, torch.int32
+    # the direct calls where torch has them: a device's tensors are there by now
+    _current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+        (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _KINDS.update({torch.float32: 0, torch.bfloat16: 1})
 
 
-def _head_rows(x, shape, what):
-    """(pointer, token stride, element type) of x [tokens, heads, head_dim],
-    whose tokens may be apart and whose heads lie one after another; shape:
-    x.shape.  (These checks are most of a small call's host time, hence one
-    look at each property.)"""
+def _stream_on(device, stream):
+    """_stream(), where the call's tensors are on `device`, which has to be the
+    current one."""
+    if device != _current():
+        raise ValueError(f"the tensors are on device {device}, which is not the current one")
+    if stream is None:
+        return _raw_stream(device)
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError(f"the stream is not of device {device}, where the tensors are")
+    return stream.cuda_stream
+
+
+def _apart(*handles):
+    return ValueError("the call's tensors are on several devices: "
+                      f"{[h.index for h in handles if h is not None]}")
+
+
+def _head_rows(x, shape, what, device):
+    """(pointer, token stride, element type) of x [tokens, heads, head_dim] on
+    `device`, whose tokens may be apart and whose heads lie one after another;
+    shape: x.shape.  (These checks are most of a small call's host time, hence
+    one look at each property.)"""
     if not _KINDS:
         _kinds()
     kind = _KINDS.get(x.dtype)
     tokens, heads, dim = shape
     step, head, one = x.stride()
-    if kind is None or not x.is_cuda or one != 1 or (head != dim and heads > 1):
+    if kind is None or device < 0 or x.get_device() != device or one != 1 or \
+            (head != dim and heads > 1):
         raise ValueError(f"{what}: expected float32 or bfloat16 [tokens, heads, head_dim] on the "
-                         "device, the heads of a token contiguous")
+                         "call's device, the heads of a token contiguous")
     return x.data_ptr(), step if tokens > 1 else heads * dim, kind
 
 
-def _cache_rows(x, cache, batch, what):
+def _cache_rows(x, cache, batch, what, device):
     """_head_rows of rows that go into the cache."""
     shape = x.shape
     if len(shape) != 3 or shape[1] != cache.kv_heads or shape[2] != cache.head_dim or \
             shape[0] < batch.n_tokens:
         raise ValueError(f"{what}: expected [{batch.n_tokens} tokens, {cache.kv_heads}, "
                          f"{cache.head_dim}], got {tuple(shape)}")
-    return _head_rows(x, shape, what)
+    return _head_rows(x, shape, what, device)
 
 
-def _bf16(t, numel, what):
-    """Pointer of a contiguous BF16 device tensor of at least numel elements, or None."""
+def _bf16(t, numel, what, device):
+    """Pointer of a contiguous BF16 tensor of at least numel elements on `device`, or None."""
     if t is None:
         return None
     if not _KINDS:
         _kinds()
-    if t.dtype is not _BF16 or not t.is_cuda or not t.is_contiguous() or t.numel() < numel:
-        raise ValueError(f"{what}: expected a contiguous bfloat16 device tensor of at least "
-                         f"{numel} elements")
+    if t.dtype is not _BF16 or t.get_device() != device or not t.is_contiguous() or \
+            t.numel() < numel:
+        raise ValueError(f"{what}: expected a contiguous bfloat16 tensor of at least {numel} "
+                         "elements on the call's device")
     return t.data_ptr()
 
 
-def _positions(t, tokens):
+def _positions(t, tokens, device):
     if t is None:
         return None
-    if t.dtype is not _I32 or not t.is_cuda or not t.is_contiguous() or t.numel() < tokens:
-        raise ValueError(f"positions: expected a contiguous int32 device tensor of at least "
-                         f"{tokens} elements")
+    if t.dtype is not _I32 or t.get_device() != device or not t.is_contiguous() or \
+            t.numel() < tokens:
+        raise ValueError(f"positions: expected a contiguous int32 tensor of at least {tokens} "
+                         "elements on the call's device")
     return t.data_ptr()
 
 
@@ -511,25 +537,29 @@ def eq_qk_norm_rope(q, k, q_out, k_out, *, q_weight=None, k_weight=None, eps: fl
     tokens, heads, dim = shape
     if tokens >> 32:
         raise ValueError("more than 2^32 - 1 tokens")
-    pq, sq, kind = _head_rows(q, shape, "q")
-    pqo = _bf16(q_out, tokens * heads * dim, "q_out")
+    dev = q.get_device()
+    pq, sq, kind = _head_rows(q, shape, "q", dev)
+    pqo = _bf16(q_out, tokens * heads * dim, "q_out", dev)
     pk = pko = None
     sk = hk = 0
     if k is not None:
         shape = k.shape
         n, hk, kd = shape
-        pk, sk, kind_k = _head_rows(k, shape, "k")
+        pk, sk, kind_k = _head_rows(k, shape, "k", dev)
         if n != tokens or kd != dim or kind_k != kind:
             raise ValueError("q and k differ in tokens, head_dim or type")
-        pko = _bf16(k_out, tokens * hk * dim, "k_out")
+        pko = _bf16(k_out, tokens * hk * dim, "k_out", dev)
     pr = None
     if rope is not None:
         if positions is None:
             raise ValueError("a rotation needs positions")
+        if rope.index != dev:
+            raise ValueError("rope is not on q's device")
         pr = rope.ptr
-    rc = lib().eq_qk_norm_rope(pq, sq, heads, _bf16(q_weight, dim, "q_weight"), pqo, pk, sk, hk,
-                               _bf16(k_weight, dim, "k_weight"), pko, kind, tokens, dim, eps,
-                               _positions(positions, tokens), pr, _stream(stream))
+    rc = lib().eq_qk_norm_rope(pq, sq, heads, _bf16(q_weight, dim, "q_weight", dev), pqo, pk, sk,
+                               hk, _bf16(k_weight, dim, "k_weight", dev), pko, kind, tokens, dim,
+                               eps, _positions(positions, tokens, dev), pr,
+                               _stream_on(dev, stream))
     if rc:
         raise EqError("eq_qk_norm_rope", rc)
 
@@ -544,11 +574,15 @@ def eq_kv_append(cache, batch, k, v, *, rope=None, positions=None, stream=None) 
     """Append k and v [n_tokens, kv_heads, head_dim] (fp32 or BF16 each), the
     keys rotated on the way when rope is given: at `positions`, or at the
     tokens' places in their sequences."""
-    pk, sk, kind_k = _cache_rows(k, cache, batch, "k")
-    pv, sv, kind_v = _cache_rows(v, cache, batch, "v")
+    dev = cache.index
+    if batch.index != dev or (rope is not None and rope.index != dev):
+        raise _apart(cache, batch, rope)
+    pk, sk, kind_k = _cache_rows(k, cache, batch, "k", dev)
+    pv, sv, kind_v = _cache_rows(v, cache, batch, "v", dev)
     rc = lib().eq_kv_append(cache.ptr, batch.ptr, pk, sk, kind_k, pv, sv, kind_v,
-                            _positions(positions, batch.n_tokens),
-                            None if rope is None else rope.ptr, _stream(stream))
+                            _positions(positions, batch.n_tokens, dev),
+                            None if rope is None else rope.ptr,
+                            _stream_on(dev, stream))
     if rc:
         raise EqError("eq_kv_append", rc)
 
@@ -557,8 +591,11 @@ def eq_kv_read(cache, batch, k, v, stream=None) -> None:
     """The cache's values of the batch's tokens, as BF16: k and v contiguous
     [n_tokens, kv_heads, head_dim]."""
     n = batch.n_tokens * cache.kv_heads * cache.head_dim
-    rc = lib().eq_kv_read(cache.ptr, batch.ptr, _bf16(k, n, "k"), _bf16(v, n, "v"),
-                          _stream(stream))
+    dev = cache.index
+    if batch.index != dev:
+        raise _apart(cache, batch)
+    rc = lib().eq_kv_read(cache.ptr, batch.ptr, _bf16(k, n, "k", dev), _bf16(v, n, "v", dev),
+                          _stream_on(dev, stream))
     if rc:
         raise EqError("eq_kv_read", rc)
 
@@ -585,14 +622,21 @@ def eq_attn_kv4(cache, batch, q, scale: float, out, ws=None, *, window: int = 0,
         raise ValueError(f"window {window}: expected 0 (none) to 2^32 - 1")
     shape = q.shape
     n, heads, dim = shape
-    pq, sq, kind = _head_rows(q, shape, "q")
+    dev = cache.index
+    if batch.index != dev:
+        raise _apart(cache, batch)
+    pq, sq, kind = _head_rows(q, shape, "q", dev)
     if kind != 1 or dim != cache.head_dim or n < batch.n_tokens:
         raise ValueError(f"q: expected bfloat16 [{batch.n_tokens} tokens, heads, "
                          f"{cache.head_dim}]")
-    po = _bf16(out, batch.n_tokens * heads * dim, "out")
-    pw, nbytes = (None, 0) if ws is None else (_dptr(ws), ws.numel() * ws.element_size())
+    po = _bf16(out, batch.n_tokens * heads * dim, "out", dev)
+    pw, nbytes = None, 0
+    if ws is not None:
+        pw, nbytes = _dptr(ws), ws.numel() * ws.element_size()
+        if ws.get_device() != dev:
+            raise ValueError("ws is not on the call's device")
     rc = lib().eq_attn_kv4(cache.ptr, batch.ptr, pq, sq, heads, scale, window, po, pw, nbytes,
-                           _stream(stream))
+                           _stream_on(dev, stream))
     if rc:
         raise EqError("eq_attn_kv4", rc)
 

@@ -83,3 +83,98 @@ def test_norm_of_more_tokens_than_32_bits_is_refused():
     q = torch.zeros(1, 1, 16).expand((1 << 32) + 1, 1, 16)
     with pytest.raises(ValueError, match="tokens"):
         eq.eq_qk_norm_rope(q, None, q, None)
+
+
+class OnDevice:
+    """What the binding looks at of a contiguous tensor on cuda:`index`."""
+    is_cuda = True
+
+    def __init__(self, shape, dtype, index):
+        torch = pytest.importorskip("torch")
+        self.shape, self.dtype, self.device = tuple(shape), dtype, torch.device("cuda", index)
+
+    def get_device(self):
+        return self.device.index
+
+    def data_ptr(self):
+        return P
+
+    def is_contiguous(self):
+        return True
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+
+def _call(which, at):
+    """One call with every part on cuda:0 but for what `at` names."""
+    torch = pytest.importorskip("torch")
+    bf, i32, f32, u8 = torch.bfloat16, torch.int32, torch.float32, torch.uint8
+
+    def t(name, shape, dtype=bf):
+        return OnDevice(shape, dtype, at.get(name, at.get("all", 0)))
+
+    def rope():
+        return eq.Rope(t("rope", (9, 32), f32), t("rope", (9, 32), f32))
+
+    class Stream:
+        cuda_stream, device_index = 0, at.get("stream", at.get("all", 0))
+
+    stream = Stream if "stream" in at else None
+    if which == "norm":
+        return eq.eq_qk_norm_rope(t("q", (4, 4, 64)), t("k", (4, 2, 64)), t("q_out", (4, 4, 64)),
+                                  t("k_out", (4, 2, 64)), q_weight=t("q_weight", (64,)),
+                                  k_weight=t("k_weight", (64,)), rope=rope(),
+                                  positions=t("positions", (4,), i32), stream=stream)
+    cache = eq.KvCache(t("cache", (3, eq.eq_kv_page_bytes(2, 64, 64)), u8), page_tokens=64, kv_heads=2,
+                       head_dim=64)
+    batch = eq.KvBatch(t("batch", (2,), i32), t("batch", (1,), i32), t("batch", (1, 3), i32),
+                       n_tokens=4, max_new=4, max_len=100)
+    if which == "append":
+        return eq.eq_kv_append(cache, batch, t("k", (4, 2, 64)), t("v", (4, 2, 64), f32), rope=rope(),
+                               positions=t("positions", (4,), i32), stream=stream)
+    if which == "read":
+        return eq.eq_kv_read(cache, batch, t("k", (4, 2, 64)), t("v", (4, 2, 64)), stream=stream)
+    return eq.eq_attn_kv4(cache, batch, t("q", (4, 4, 64)), 0.125, t("out", (4, 4, 64)),
+                          t("ws", (1 << 20,), u8), stream=stream)
+
+
+@pytest.mark.parametrize("which,part", [("norm", p) for p in (
+    "q", "k", "q_out", "k_out", "q_weight", "k_weight", "rope", "positions", "stream", "all")] + [
+    ("append", p) for p in ("cache", "batch", "k", "v", "rope", "positions", "stream", "all")] + [
+    ("read", p) for p in ("cache", "batch", "k", "v", "stream", "all")] + [
+    ("attn", p) for p in ("cache", "batch", "q", "out", "ws", "stream", "all")])
+def test_tensors_that_are_not_on_the_current_device_are_refused(which, part, monkeypatch):
+    """A kernel would follow another device's addresses."""
+    torch = pytest.importorskip("torch")
+    eq._kinds()
+    monkeypatch.setattr(eq, "_current", lambda: 0)
+    monkeypatch.setattr(eq, "_raw_stream", lambda device: 0)
+    called = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(real, name) if name == "eq_kv_page_bytes" else lambda *a: called.append(name) or 0
+
+    real = eq.lib()
+    monkeypatch.setattr(eq, "_lib", Lib())
+    _call(which, {})
+    assert len(called) == 1
+    with pytest.raises(ValueError, match="device"):
+        _call(which, {part: 1})
+    assert len(called) == 1
+
+
+def test_tables_on_two_devices_are_refused():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError, match="device"):
+        eq.Rope(OnDevice((9, 32), torch.float32, 0), OnDevice((9, 32), torch.float32, 1))
