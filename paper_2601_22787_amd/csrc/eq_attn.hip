@@ -1033,7 +1033,7 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
   const bool one_page = cache->page_tokens >= kTile;
   const bool pair = pair_columns(batch->max_new, group);
   const bool stream_codes = stream_cache(p, batch->n_seqs, cache->kv_heads, cache->head_dim,
-                                         batch->max_len);
+                                         batch->max_new, batch->max_len, window);
   if (cache->head_dim == 128) launch_attn<128>(a, p, pair, one_page, stream_codes, grid, join, stream);
   else launch_attn<64>(a, p, pair, one_page, stream_codes, grid, join, stream);
   return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP;

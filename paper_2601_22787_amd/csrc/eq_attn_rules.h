@@ -84,12 +84,15 @@ inline bool pair_columns(uint32_t max_new, uint32_t group) {
 }
 
 // Codes that are read once in all, and more of them than the memory-side cache
-// holds (256 MiB), pass the caches as streams: 284 000 tokens of 8 heads 74 ->
-// 70 us.  Smaller caches stay in it between calls (16 MiB: 7.5 us, as streams
-// 8.1), and query tiles share what the first of them has read.
+// keeps, pass the caches as streams: 303 MB of 8 heads 74 -> 70 us.  Fewer stay in
+// it between calls (16 MiB: 7.5 us, as streams 8.1), and query tiles share what the
+// first of them has read.  The limit is three quarters of its 256 MiB: the call's
+// other data pass through it too.  max_len and the window bound what is read.
 inline bool stream_cache(const Plan &p, uint32_t n_seqs, uint32_t kv_heads, uint32_t head_dim,
-                         uint32_t max_len) {
-  return p.q_tiles == 1 && uint64_t(n_seqs) * max_len * kv_heads * (head_dim + head_dim / 32 + 1) >
+                         uint32_t max_new, uint32_t max_len, uint32_t window) {
+  const uint64_t tokens =
+      window ? std::min<uint64_t>(max_len, uint64_t(window) + max_new - 1) : max_len;
+  return p.q_tiles == 1 && n_seqs * tokens * kv_heads * (head_dim + head_dim / 32 + 1) >
                                uint64_t(192) << 20;
 }
 

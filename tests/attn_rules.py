@@ -34,7 +34,8 @@ def plan(n_seqs, kv_heads, group, max_new, max_len, window, dim):
         if not prompt and seen <= short:
             ct = four(seen)
         chunks = max(1, _up(seen, ct))
-    read = n_seqs * max_len * kv_heads * (dim + dim // 32 + 1)
+    tokens = min(max_len, window + max_new - 1) if window else max_len
+    read = n_seqs * tokens * kv_heads * (dim + dim // 32 + 1)
     return Plan(prompt, width, tile, q_tiles, chunks, ct, cols <= 8, q_tiles == 1 and read > 192 << 20)
 
 

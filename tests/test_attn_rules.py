@@ -23,7 +23,7 @@ int main() {
   }
 }
 """
-STREAM = "eq_attn::stream_cache(p, v[0], v[1], v[6], v[4])"
+STREAM = "eq_attn::stream_cache(p, v[0], v[1], v[6], v[3], v[4], v[5])"
 
 
 @pytest.fixture(scope="module")
@@ -73,3 +73,10 @@ def test_every_seen_token_is_in_a_chunk(rules):
             at = attn_rules.spans(p, group, count, kv_len, max_len, window)
             assert len(at) <= p.q_tiles
             assert max(b - a for a, b in at) <= p.chunks * p.chunk_tiles, (row, count, kv_len)
+
+
+def test_codes_that_a_window_leaves_out_are_not_counted(rules):
+    """16 sequences of 8 heads of 128, bounded by 32768 tokens: 558 MB of codes,
+    of which windows of 512 leave 9 MB and of 16384 279 MB."""
+    got = rules([(16, 8, 8, 1, 32768, w, 128) for w in (0, 512, 1 << 14, 1 << 15, (1 << 32) - 1)])
+    assert [p.stream for p in got] == [1, 0, 1, 1, 1]
