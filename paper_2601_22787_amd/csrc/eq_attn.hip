@@ -601,8 +601,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[3 * kBuf];
   const View &w = a.w;
   const uint32_t s = blockIdx.y;
-  // heads first (the blocks of a head on one XCD, whose L2 then holds its
-  // cache), and a sequence's last queries, which see most, before its first
+  // heads first (blocks go round the 8 XCDs, so with a multiple of 8 heads those of
+  // a head share one, whose L2 then holds its cache), and a sequence's last
+  // queries, which see most, before its first
   const uint32_t h = blockIdx.x % w.kv_heads, rest = blockIdx.x / w.kv_heads;
   const uint32_t chunk = rest % a.chunks, qt = a.q_tiles - 1 - rest / a.chunks;
   const Seq q = sequence(w, s);
@@ -622,12 +623,12 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
            : nullptr;
   PromptQuery<D> query;
   query.load(row, half);
-  // the wavefront's own span: tokens that some column, and that every one sees
-  int32_t w_lo = 0, w_hi = 0, all_lo = 0, all_hi = 0;
+  // tokens in [all_lo, all_hi) are seen by every column of the wavefront (the block's
+  // tiles are multiplied whole, also those that none of them sees)
+  int32_t all_lo = 0, all_hi = 0;
   if (wave_col < sp.cols) {
     const int32_t p0 = q.base + int32_t(wave_col / a.group);
     const int32_t p1 = q.base + int32_t((min(wave_col + 32, sp.cols) - 1) / a.group);
-    w_lo = start_of(a.window, p0), w_hi = end_of(q, p1);
     all_lo = start_of(a.window, p1), all_hi = end_of(q, p0);
   }
 
