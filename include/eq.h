@@ -393,11 +393,14 @@ size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *
  * elements apart, 16-byte aligned rows; out: BF16, contiguous, 16-byte
  * aligned.  The new tokens' keys and values are in the cache already
  * (eq_kv_append first).  scale > 0.  Scores, softmax statistics and sums are in
- * fp32; queries enter exactly where at least 2^-14 of the largest of their 32
- * channels (smaller ones within 2^-21 of it), P with 8 significant bits.  A query
- * with an infinity or NaN, and one that sees such a key or value, gives NaN.  ws/ws_bytes: at least
- * eq_attn_kv4_workspace_bytes(), 16-byte aligned; nothing in it is kept
- * between calls.  Sums are added in a fixed order. */
+ * fp32.  Queries enter exactly where at least 2^-14 of the largest of their 32
+ * channels, smaller ones within 2^-22 of it.  P times its value's scale enters
+ * with 8 significant bits; where prompt tiles are not used (few new tokens), only
+ * down to 2^-14 of the largest such product of 128 tokens, and smaller ones are
+ * within 2^-22 of that.  A query with an infinity or NaN, and one that sees such a
+ * key or value, gives NaN.  ws/ws_bytes: at least eq_attn_kv4_workspace_bytes(),
+ * 16-byte aligned; nothing in it is kept between calls.  Sums are added in a fixed
+ * order. */
 int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
                 uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window, uint16_t *out,
                 void *ws, size_t ws_bytes, hipStream_t stream);
