@@ -405,6 +405,96 @@ int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16
                 uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window, uint16_t *out,
                 void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Drafted trees.  A sequence's rows of a call are then the nodes of a tree: row
+ * seq_start[s] + i is node i, and parents[row] its parent, an earlier node, or -1
+ * for the sequence's tokens before the call.  Node 0 is the last token that was
+ * accepted, whose key and value are not in the cache yet; the others are drafted
+ * behind it.  Nodes are cached at consecutive places (kv_len counts them), but stand
+ * at positions kv_len - nodes + depth.  One step of speculative decoding:
+ *   eq_tree_mask            masks and positions, for all layers
+ *   each layer              eq_qk_norm_rope and eq_kv_append at those positions,
+ *                           eq_attn_kv4_tree
+ *   eq_tree_verify          which path is kept, and the token behind it
+ *   eq_kv_keep              the path's keys and values to consecutive places, in all
+ *                           layers' caches
+ * A chain of drafted tokens is a tree of one path.  All of it is on the device and may
+ * be captured; max_new is at most EQ_TREE_NODES. */
+#define EQ_TREE_NODES 256
+
+/* Masks and positions of trees.  mask: [n_tokens][W] words, W = ceil(max_new / 32)
+ * (device); bit j % 32 of word j / 32 is set where j is the node itself or one of its
+ * ancestors, with window > 0 the nearest `window` of those.  positions: int32
+ * [n_tokens].  A node whose parent is no earlier node (and not -1), and those behind
+ * it, are left out: mask 0, position -1.  Of the batch only seq_start, kv_len, n_seqs,
+ * n_tokens and max_new are looked at; rows of no sequence are left as they are. */
+int eq_tree_mask(const eq_kv_batch *batch, const int32_t *parents, uint32_t window, uint32_t *mask,
+                 int32_t *positions, hipStream_t stream);
+
+/* Workspace bytes of eq_attn_kv4_tree (0 when it needs none, or on bad arguments). */
+size_t eq_attn_kv4_tree_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
+                                        uint32_t q_heads);
+
+/* eq_attn_kv4 with a mask for the new tokens: a row sees the cached tokens before the
+ * sequence's new ones, with window > 0 those at places above positions[row] - window
+ * (positions below the first new place count as that; NULL without a window), and of
+ * the new ones those of its bits (mask: [n_tokens][W] as above; any bits, not a tree's
+ * alone; the window is not looked at for them).  A row without any bit sees nothing:
+ * zeros.  Types, precision, alignment and workspace as for eq_attn_kv4. */
+int eq_attn_kv4_tree(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
+                     uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
+                     const uint32_t *mask, const int32_t *positions, uint16_t *out, void *ws,
+                     size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of eq_tree_verify (0 on bad arguments); draft: whether it gets the
+ * draft's logits. */
+size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, int draft);
+
+/* Verification of drafted tokens, so that what is kept is distributed as the target's
+ * own tokens.  tokens[row]: a node's token.  target: n_tokens rows of `vocab` logits
+ * (EQ_F32 or EQ_BF16, target_stride elements apart, any alignment), row i those behind
+ * node i; draft: likewise, those that node i's children were drawn from, one after
+ * another in the order of their rows, without replacement or (replace) with; or NULL,
+ * where the children were not drawn (a table's, the most likely ones).  p and q are
+ * their softmax at temperature[s] (NULL: 1).
+ * From node 0 on, a node's children are tested in turn: child x is accepted where
+ * random[its row] q(x) < p(x); else p becomes max(p - q, 0), normalised, q without
+ * replacement loses x and is normalised, and the next is tested.  (Without a draft: x
+ * is accepted where random < p(x), else p loses x.)  The accepted child is next.  Where
+ * none is, the token behind the path is the first at which the running sum of what is
+ * left of p, in the tokens' order, passes random[row of node 0] times the whole (of
+ * p itself, where nothing is left).  random: fp32, taken into [0, 1 - 2^-24] (NaN: 0).
+ * A temperature that is not above 0: the child that is the target's largest logit is
+ * accepted, the lowest of equal ones; random and draft are not looked at.
+ * path: the kept nodes of each sequence from its first row on, node 0 first, then -1;
+ * kept[s]: their number (0 for a sequence without rows); next[s]: the token behind
+ * them, or -1 where a row of logits that is looked at holds a NaN or +infinity or
+ * nothing above -infinity (the path up to there is kept).  Tokens outside the
+ * vocabulary are never accepted, nor nodes that are not their parent's later rows.
+ * All in 64 bits: tokens are those of exact arithmetic but where a random number is
+ * within about 2^-45 of a border.  max_children bounds a node's children (1: a
+ * chain); with more than that, results are the same, and slower.  vocab is at most
+ * 2^24.  ws/ws_bytes: at least eq_tree_verify_workspace_bytes(), 16-byte aligned;
+ * nothing in it is kept between calls. */
+int eq_tree_verify(const eq_kv_batch *batch, const int32_t *parents, const int32_t *tokens,
+                   const void *target, uint64_t target_stride, uint32_t target_dtype,
+                   const void *draft, uint64_t draft_stride, uint32_t draft_dtype, uint32_t vocab,
+                   const float *temperature, const float *random, uint32_t replace,
+                   uint32_t max_children, int32_t *path, int32_t *kept, int32_t *next, void *ws,
+                   size_t ws_bytes, hipStream_t stream);
+
+/* Keep a path: in each of n caches (host array, 1 to EQ_KEEP_CACHES, of one size and
+ * without common pages, read by the batch's page table), the k-th of a sequence's new
+ * places takes the key and value of new token path[seq_start[s] + k], for k < kept[s].
+ * Entries below k or beyond the sequence's rows, and tokens of pages that are not
+ * there, are left out.  Places behind the kept ones hold what they held.  new_len (or
+ * NULL; not kv_len itself, which other blocks read): int32 [n_seqs], kv_len less the
+ * nodes that were not kept.  Two sequences may share pages, but not 8 aligned positions
+ * that either moves tokens to. */
+#define EQ_KEEP_CACHES 128
+int eq_kv_keep(const eq_kv_cache *const *caches, uint32_t n, const eq_kv_batch *batch,
+               const int32_t *path, const int32_t *kept, int32_t *new_len, hipStream_t stream);
+
 /* Wait for `stream`, then report EQ_ECORRUPT if any decode since the last
  * eq_layer_prepare found a chunk whose stream or terminal states did not
  * check out, else EQ_OK (or EQ_EHIP). */

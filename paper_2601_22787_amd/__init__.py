@@ -114,6 +114,17 @@ SIGNATURES = {
     "eq_attn_kv4_workspace_bytes": (ctypes.c_size_t, [_vp, _vp, ctypes.c_uint32]),
     "eq_attn_kv4": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, ctypes.c_uint32, ctypes.c_float,
                                    ctypes.c_uint32, _vp, _vp, ctypes.c_size_t, _vp]),
+    "eq_tree_mask": (ctypes.c_int, [_vp, _vp, ctypes.c_uint32, _vp, _vp, _vp]),
+    "eq_attn_kv4_tree_workspace_bytes": (ctypes.c_size_t, [_vp, _vp, ctypes.c_uint32]),
+    "eq_attn_kv4_tree": (ctypes.c_int, [_vp, _vp, _vp, ctypes.c_uint64, ctypes.c_uint32,
+                                        ctypes.c_float, ctypes.c_uint32, _vp, _vp, _vp, _vp,
+                                        ctypes.c_size_t, _vp]),
+    "eq_tree_verify_workspace_bytes": (ctypes.c_size_t, [_vp, ctypes.c_uint32, ctypes.c_int]),
+    "eq_tree_verify": (ctypes.c_int, [_vp, _vp, _vp, _vp, ctypes.c_uint64, ctypes.c_uint32, _vp,
+                                      ctypes.c_uint64, ctypes.c_uint32, ctypes.c_uint32, _vp, _vp,
+                                      ctypes.c_uint32, ctypes.c_uint32, _vp, _vp, _vp, _vp,
+                                      ctypes.c_size_t, _vp]),
+    "eq_kv_keep": (ctypes.c_int, [_vp, ctypes.c_uint32, _vp, _vp, _vp, _vp, _vp]),
     "eq_get_status": (ctypes.c_int, [ctypes.POINTER(eq_layer), _vp]),
     "eq_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "eqe_alpha_search": (ctypes.c_float, [_vp, ctypes.c_uint32, ctypes.c_uint32, ctypes.c_double,
@@ -444,17 +455,33 @@ class KvBatch:
                                _dptr(page_table, torch.int32), n, page_table.shape[1], n_tokens,
                                max_new, max_len)
         self.ptr = ctypes.addressof(self.raw)
-        self.n_tokens = n_tokens
+        self.n_tokens, self.n_seqs, self.max_new = n_tokens, n, max_new
+        self.mask_words = -(-max_new // 32)  # of a drafted tree's masks
+
+
+class KvCaches:
+    """Caches of one size on one device, such as a model's layers', that
+    eq_kv_keep treats alike."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        if not self.caches:
+            raise ValueError("no caches")
+        self.index = self.caches[0].index
+        if any(c.index != self.index for c in self.caches):
+            raise _apart(*self.caches)
+        self.array = (_vp * len(self.caches))(*(c.ptr for c in self.caches))
+        self.ptr = ctypes.addressof(self.array)
 
 
 _KINDS = {}  # torch dtype -> EQ_F32 or EQ_BF16, filled by the first call
-_BF16 = _I32 = _current = _raw_stream = None
+_BF16 = _I32 = _F32 = _current = _raw_stream = None
 
 
 def _kinds():
-    global _BF16, _I32, _current, _raw_stream
+    global _BF16, _I32, _F32, _current, _raw_stream
     import torch
-    _BF16, _I32 = torch.bfloat16, torch.int32
+    _BF16, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
     # the direct calls where torch has them: a device's tensors are there by now
     _current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
@@ -639,6 +666,167 @@ def eq_attn_kv4(cache, batch, q, scale: float, out, ws=None, *, window: int = 0,
                            _stream_on(dev, stream))
     if rc:
         raise EqError("eq_attn_kv4", rc)
+
+
+# ---------------------------------------------------------------- drafted trees
+def _ints(t, numel, what, device, dtype=None):
+    """Pointer of a contiguous int32 (or dtype) tensor of at least numel elements on
+    `device`, or None."""
+    if t is None:
+        return None
+    if not _KINDS:
+        _kinds()
+    if t.dtype is not (dtype or _I32) or t.get_device() != device or not t.is_contiguous() or \
+            t.numel() < numel:
+        raise ValueError(f"{what}: expected a contiguous {dtype or _I32} tensor of at least {numel} "
+                         "elements on the call's device")
+    return t.data_ptr()
+
+
+def _workspace(ws, device):
+    if ws is None:
+        return None, 0
+    if ws.get_device() != device:
+        raise ValueError("ws is not on the call's device")
+    return _dptr(ws), ws.numel() * ws.element_size()
+
+
+def _logit_rows(x, batch, vocab, what, device):
+    """(pointer, row stride, element type) of logits [n_tokens, vocab]."""
+    if not _KINDS:
+        _kinds()
+    kind = _KINDS.get(x.dtype)
+    if kind is None or x.get_device() != device or x.dim() != 2 or x.shape[0] < batch.n_tokens or \
+            x.shape[1] != vocab or (x.stride(1) != 1 and vocab > 1):
+        raise ValueError(f"{what}: expected float32 or bfloat16 [{batch.n_tokens} rows, {vocab}] on the "
+                         "call's device, a row's logits one after another")
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else vocab, kind
+
+
+def tree_buffers(batch):
+    """(mask, positions) for eq_tree_mask: int32 [n_tokens, words] and [n_tokens]."""
+    import torch
+    return (torch.empty(batch.n_tokens, batch.mask_words, dtype=torch.int32, device=batch.device),
+            torch.empty(batch.n_tokens, dtype=torch.int32, device=batch.device))
+
+
+def eq_tree_mask(batch, parents, mask, positions, *, window: int = 0, stream=None) -> None:
+    """The masks (int32 [n_tokens, batch.mask_words], a bit for each new token that
+    a node sees) and positions (int32 [n_tokens]) of the batch's trees, from each
+    node's parent among its sequence's earlier ones (-1: the cached tokens)."""
+    if window >> 32:  # (below 0 too)
+        raise ValueError(f"window {window}: expected 0 (none) to 2^32 - 1")
+    dev, n = batch.index, batch.n_tokens
+    rc = lib().eq_tree_mask(batch.ptr, _ints(parents, n, "parents", dev), window,
+                            _ints(mask, n * batch.mask_words, "mask", dev),
+                            _ints(positions, n, "positions", dev), _stream_on(dev, stream))
+    if rc:
+        raise EqError("eq_tree_mask", rc)
+
+
+def eq_attn_kv4_tree_workspace_bytes(cache, batch, q_heads: int) -> int:
+    if q_heads >> 32:
+        return 0
+    return lib().eq_attn_kv4_tree_workspace_bytes(cache.ptr, batch.ptr, q_heads)
+
+
+def attn_tree_workspace(cache, batch, q_heads: int):
+    """A device workspace for eq_attn_kv4_tree (None when it needs none)."""
+    import torch
+    n = eq_attn_kv4_tree_workspace_bytes(cache, batch, q_heads)
+    return torch.empty(n, dtype=torch.uint8, device=cache.device) if n else None
+
+
+def eq_attn_kv4_tree(cache, batch, q, scale: float, mask, out, ws=None, *, positions=None,
+                     window: int = 0, stream=None) -> None:
+    """eq_attn_kv4 where each row of q sees, of its sequence's new tokens, those of
+    its bits in `mask` (int32 [n_tokens, batch.mask_words]); with window, the cached
+    tokens above positions[row] - window."""
+    if window >> 32:  # (below 0 too)
+        raise ValueError(f"window {window}: expected 0 (none) to 2^32 - 1")
+    shape = q.shape
+    n, heads, dim = shape
+    dev = cache.index
+    if batch.index != dev:
+        raise _apart(cache, batch)
+    pq, sq, kind = _head_rows(q, shape, "q", dev)
+    if kind != 1 or dim != cache.head_dim or n < batch.n_tokens:
+        raise ValueError(f"q: expected bfloat16 [{batch.n_tokens} tokens, heads, "
+                         f"{cache.head_dim}]")
+    po = _bf16(out, batch.n_tokens * heads * dim, "out", dev)
+    pw, nbytes = _workspace(ws, dev)
+    rc = lib().eq_attn_kv4_tree(cache.ptr, batch.ptr, pq, sq, heads, scale, window,
+                                _ints(mask, batch.n_tokens * batch.mask_words, "mask", dev),
+                                _positions(positions, batch.n_tokens, dev), po, pw, nbytes,
+                                _stream_on(dev, stream))
+    if rc:
+        raise EqError("eq_attn_kv4_tree", rc)
+
+
+def eq_tree_verify_workspace_bytes(batch, vocab: int, draft: bool) -> int:
+    if vocab >> 32:
+        return 0
+    return lib().eq_tree_verify_workspace_bytes(batch.ptr, vocab, int(bool(draft)))
+
+
+def verify_workspace(batch, vocab: int, *, draft: bool = True):
+    """A device workspace for eq_tree_verify, with a draft's logits or without."""
+    import torch
+    return torch.empty(eq_tree_verify_workspace_bytes(batch, vocab, draft), dtype=torch.uint8,
+                       device=batch.device)
+
+
+def eq_tree_verify(batch, parents, tokens, target, draft, random, path, kept, next_token, ws, *,
+                   temperature=None, replace: bool = False, max_children: int = 256,
+                   stream=None) -> None:
+    """Verify the batch's drafted tokens against the target's logits [n_tokens, vocab]
+    (fp32 or BF16): the kept nodes of each sequence to path (int32 [n_tokens], -1
+    behind them), their number to kept and the token behind them to next_token (int32
+    [n_seqs]).  draft: the logits that nodes' children were drawn from, without
+    replacement unless `replace`, or None where they were not drawn.  random: fp32
+    [n_tokens] in [0, 1).  temperature: fp32 [n_seqs], 0 for the largest logit.
+    max_children: a bound of a node's children, 1 for chains."""
+    if max_children < 1 or max_children >> 32:
+        raise ValueError(f"max_children {max_children}: expected 1 to 2^32 - 1")
+    dev, n = batch.index, batch.n_tokens
+    if target.dim() != 2 or target.shape[1] >> 32:
+        raise ValueError("target: expected [rows, vocab]")
+    vocab = target.shape[1]
+    pt, st, kt = _logit_rows(target, batch, vocab, "target", dev)
+    pd = None
+    sd = kd = 0
+    if draft is not None:
+        pd, sd, kd = _logit_rows(draft, batch, vocab, "draft", dev)
+    pw, nbytes = _workspace(ws, dev)
+    rc = lib().eq_tree_verify(batch.ptr, _ints(parents, n, "parents", dev),
+                              _ints(tokens, n, "tokens", dev), pt, st, kt, pd, sd, kd, vocab,
+                              _ints(temperature, batch.n_seqs, "temperature", dev, _F32),
+                              _ints(random, n, "random", dev, _F32), int(bool(replace)),
+                              max_children, _ints(path, n, "path", dev),
+                              _ints(kept, batch.n_seqs, "kept", dev),
+                              _ints(next_token, batch.n_seqs, "next_token", dev), pw, nbytes,
+                              _stream_on(dev, stream))
+    if rc:
+        raise EqError("eq_tree_verify", rc)
+
+
+def eq_kv_keep(caches, batch, path, kept, new_len=None, *, stream=None) -> None:
+    """Keep a path: in every cache (KvCaches, a list of KvCache, or one) the k-th of a
+    sequence's new places takes new token path[seq_start + k], k < kept; new_len
+    (int32 [n_seqs], not the batch's kv_len): the lengths without what was not kept."""
+    if isinstance(caches, KvCache):
+        caches = KvCaches([caches])
+    elif not isinstance(caches, KvCaches):
+        caches = KvCaches(caches)
+    dev = caches.index
+    if batch.index != dev:
+        raise _apart(caches, batch)
+    rc = lib().eq_kv_keep(caches.ptr, len(caches.caches), batch.ptr,
+                          _ints(path, batch.n_tokens, "path", dev),
+                          _ints(kept, batch.n_seqs, "kept", dev),
+                          _ints(new_len, batch.n_seqs, "new_len", dev), _stream_on(dev, stream))
+    if rc:
+        raise EqError("eq_kv_keep", rc)
 
 
 # ---------------------------------------------------------------- encoder ABI

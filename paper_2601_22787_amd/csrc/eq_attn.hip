@@ -50,6 +50,9 @@ struct AttnArgs {
   uint32_t window;
   uint32_t q_tiles, chunks, chunk_tiles;
   float c;           // scale log2 e
+  const uint32_t *mask;      // trees: [n_tokens][mask_words], bit j: new token j is seen
+  const int32_t *positions;  // trees with a window: [n_tokens]
+  uint32_t mask_words;
 };
 
 // Columns [col0, col0 + COLS) of a sequence, and the cached tokens they see.
@@ -66,11 +69,21 @@ __device__ inline int32_t start_of(uint32_t window, int32_t pos) {
   return window && pos >= 0 && uint32_t(pos) >= window ? pos + 1 - int32_t(window) : 0;
 }
 
-template <uint32_t COLS, uint32_t TILE>
+// TREE: all columns see the tokens before the new ones (what a window hides of them
+// and lanes without a node are the kernels' own), and new ones by their masks.
+template <uint32_t COLS, uint32_t TILE, bool TREE>
 __device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
   Span p{};
   p.cols = uint32_t(q.count) * a.group;
   if (col0 >= p.cols) return p;
+  if constexpr (TREE) {
+    p.hi_min = min(max(q.base, 0), q.len);
+    p.seen = uint32_t(q.len);
+    p.first = uint32_t(start_of(a.window, max(q.base, 0))) / TILE;
+    p.last = max((p.seen + TILE - 1) / TILE, p.first);
+    p.chunks = min((p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles, a.chunks);
+    return p;
+  }
   const int32_t pos0 = q.base + int32_t(col0 / a.group);
   const int32_t pos1 = q.base + int32_t((min(col0 + COLS, p.cols) - 1) / a.group);
   p.hi_min = end_of(q, pos0);
@@ -80,6 +93,40 @@ __device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
   p.last = max((p.seen + TILE - 1) / TILE, p.first);
   p.chunks = min((p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles, a.chunks);
   return p;
+}
+
+// A tree's column: the cached tokens [lo, hi) that it sees, and its bits of new ones.
+struct Node {
+  const uint32_t *mask;  // readable for every lane
+  int32_t lo, hi, base;
+  bool alive;            // a node, which sees itself at least
+};
+
+__device__ inline Node node_of(const AttnArgs &a, const Seq &q, uint32_t token, bool real) {
+  Node n{a.mask, 0, 0, q.base, false};
+  if (!real || q.base + int32_t(token) < 0) return n;
+  const uint64_t row = uint64_t(q.row) + token;
+  n.mask += row * a.mask_words;
+  uint32_t any = 0;
+  for (uint32_t i = 0; i < a.mask_words; ++i) any |= n.mask[i];
+  if (!any) return n;
+  n.alive = true;
+  n.hi = min(max(q.base, 0), q.len);
+  if (a.window) n.lo = min(start_of(a.window, max(a.positions[row], max(q.base, 0))), n.hi);
+  return n;
+}
+
+// Word i of a column's mask, 0 outside it.
+__device__ inline uint32_t mask_word(const AttnArgs &a, const uint32_t *mask, int32_t i) {
+  const uint32_t w = mask[min(max(i, 0), int32_t(a.mask_words) - 1)];
+  return uint32_t(i) < a.mask_words ? w : 0u;
+}
+
+// The largest x of a wavefront.
+__device__ inline int32_t wave_max(int32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = max(x, __shfl_xor(x, d));
+  return x;
 }
 
 // x / scale as two E4M3 terms, of four values: h at `scale`, l at scale / 32 (what h
@@ -237,7 +284,9 @@ __device__ inline int4v load_codes(const uint8_t *p) {
 // bound by the chain of one tile (page number, codes, two products with the
 // softmax between): 512 tokens of 32 heads 5.6 us, 8 x 4096 tokens 13.3 with the
 // join.
-template <int D, bool ONE, bool STREAM, bool PAIR>
+//
+// TREE: a column's new tokens are its mask's, 16 bits of it for 16 tokens in a row.
+template <int D, bool ONE, bool STREAM, bool PAIR, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int ND = D / 16;
   constexpr uint32_t kStride = D + 4;  // floats a column in LDS
@@ -253,7 +302,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
   const uint32_t col = lane & 15, g = lane >> 4;
   const Seq q = sequence(w, s);
-  const Span sp = span_of<kCols, kTile>(a, q, col0);
+  const Span sp = span_of<kCols, kTile, TREE>(a, q, col0);
 
   // Page numbers of a tile's four 32-token units (one page when it holds them
   // all), by scalar loads.  The table is read up to its width, not up to the
@@ -288,7 +337,15 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const bool real = index < sp.cols;
   const uint32_t token = index / a.group;
   const int32_t pos = q.base + int32_t(token);
-  const int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
+  int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
+  int32_t hi_min = sp.hi_min, lo_max = sp.lo_max;
+  Node node{};
+  if constexpr (TREE) {
+    node = node_of(a, q, token, real);
+    hi = node.hi, lo = node.lo;
+    if (__any(real && !node.alive)) hi_min = 0;
+    if (a.window) lo_max = wave_max(lo);
+  }
 
   // a lane's parts of a tile: keys of units gk/2 and 2 + gk/2, values of unit g,
   // value scales of units g/2 and 2 + g/2
@@ -305,6 +362,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   int4v kreg[8], vreg[ND];
   uint4 va, vb;  // (PAIR: va is of the lane's own 16 tokens)
   int ksa, ksb;
+  uint32_t ma[2] = {}, mb[2] = {};  // TREE: mask words of va's and vb's tokens
   auto load_k = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const pa = part_of(d, gk >> 1), *const pb = part_of(d, 2 + (gk >> 1));
     const uint32_t a0 = slot_of(tile, gk >> 1) + 16 * (gk & 1);
@@ -323,6 +381,12 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     va = *reinterpret_cast<const uint4 *>(part_of(d, unit) + (at + slot_of(tile, unit)));
     if constexpr (!PAIR)
       vb = *reinterpret_cast<const uint4 *>(part_of(d, 2 + unit) + (at + slot_of(tile, 2 + unit)));
+    if constexpr (TREE) {
+      const int32_t i = (int32_t(tile * kTile + 16 * g) + (upper ? 64 : 0) - node.base) >> 5;
+      ma[0] = mask_word(a, node.mask, i), ma[1] = mask_word(a, node.mask, i + 1);
+      if constexpr (!PAIR)
+        mb[0] = mask_word(a, node.mask, i + 2), mb[1] = mask_word(a, node.mask, i + 3);
+    }
   };
   auto load_v = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const p = part_of(d, g) + (w.v_off + slot_of(tile, g) * (D / 2) + col * 16);
@@ -375,7 +439,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
 #pragma unroll
       for (uint32_t u = 0; u < (ONE ? 1 : 4); ++u) gone |= uint32_t(ids.u[u] >= w.n_pages) << u;
       if (ONE && gone) gone = 15;
-      const bool masked = at + int32_t(kTile) > sp.hi_min || at < sp.lo_max || gone;
+      const bool masked = at + int32_t(kTile) > hi_min || at < lo_max || gone;
       // a lane's scores: all 32 of its tokens, or, with PAIR, 16 of them and the
       // sum of both terms, whose other half the lane 8 columns on holds
       constexpr int NS = PAIR ? 16 : 32;
@@ -393,14 +457,20 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
       }
       uint32_t visible = ~0u;  // bit i: this lane's column sees token i of them
       if (masked) {
-        auto bits = [&](uint32_t unit, int32_t from) {  // of 16 tokens
+        auto bits = [&](uint32_t unit, int32_t from, const uint32_t (&m)[2]) {  // of 16 tokens
           const int32_t u = min(max(lo - from, 0), 16), v = min(max(hi - from, u), 16);
-          return gone >> unit & 1 ? 0u : (1u << v) - (1u << u);
+          uint32_t b = (1u << v) - (1u << u);
+          if constexpr (TREE) {
+            const int32_t there = min(max(int32_t(sp.seen) - from, 0), 16);
+            const uint32_t own = __builtin_amdgcn_alignbit(m[1], m[0], uint32_t(from - node.base) & 31);
+            b |= node.alive ? own & ((1u << there) - 1) : 0u;
+          }
+          return gone >> unit & 1 ? 0u : b;
         };
         const uint32_t unit = (g >> 1) + (upper ? 2 : 0);
         const int32_t from = at + 16 * int32_t(g) + (upper ? 64 : 0);
-        visible = bits(unit, from);
-        if constexpr (!PAIR) visible |= bits(2 + unit, from + 64) << 16;
+        visible = bits(unit, from, ma);
+        if constexpr (!PAIR) visible |= bits(2 + unit, from + 64, mb) << 16;
 #pragma unroll
         for (int i = 0; i < NS; ++i)
           x[i] = __uint_as_float((__float_as_uint(x[i]) & bit_mask(visible, i)) |
@@ -597,7 +667,7 @@ struct PromptQuery {
 // of w P as E4M3 (278: registers spill), 8 wavefronts in two halves that take
 // turns (202), value codes brought to BF16 by each wavefront (201 against 197), 3
 // wavefronts a SIMD with the queries in LDS (272).
-template <int D>
+template <int D, bool TREE>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   constexpr int ND = D / 32, KK = D / 64;
   constexpr uint32_t kRow = D / 2 + 16;  // bytes a key in LDS: 16 rows start in 16 banks
@@ -614,7 +684,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   const uint32_t chunk = rest % a.chunks, qt = a.q_tiles - 1 - rest / a.chunks;
   const Seq q = sequence(w, s);
   const uint32_t col0 = qt * kPromptCols;
-  const Span sp = span_of<kPromptCols, kPromptTile>(a, q, col0);
+  const Span sp = span_of<kPromptCols, kPromptTile, TREE>(a, q, col0);
   if (col0 >= sp.cols || chunk >= max(sp.chunks, 1u)) return;
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = eq_dev::uniform(tid >> 6);
   const uint32_t col = lane & 31, half = lane >> 5;
@@ -623,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   const bool real = index < sp.cols;
   const uint32_t token = index / a.group;
   const int32_t pos = q.base + int32_t(token);
-  const int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
+  int32_t hi = real ? end_of(q, pos) : 0, lo = real ? start_of(a.window, pos) : 0;
   const uint16_t *const row =
       real ? a.q + uint64_t(q.row + token) * a.q_stride + uint64_t(h * a.group + index % a.group) * D
            : nullptr;
@@ -636,6 +706,13 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
     const int32_t p0 = q.base + int32_t(wave_col / a.group);
     const int32_t p1 = q.base + int32_t((min(wave_col + 32, sp.cols) - 1) / a.group);
     all_lo = start_of(a.window, p1), all_hi = end_of(q, p0);
+  }
+  Node node{};
+  if constexpr (TREE) {
+    node = node_of(a, q, token, real);
+    hi = node.hi, lo = node.lo;
+    all_hi = __any(real && !node.alive) ? 0 : sp.hi_min;
+    all_lo = a.window ? wave_max(lo) : 0;
   }
 
   // staging: D threads copy a unit, 16 bytes of its key codes, 16 of its value
@@ -742,11 +819,19 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint32_t gone = u ? odd.z : odd.x, nan = u ? odd.w : odd.y;
+        uint32_t own = 0;  // TREE: the unit's new tokens that are seen
+        if constexpr (TREE) {
+          const int32_t from = at + 32 * u - node.base, there = int32_t(sp.seen) - at - 32 * u;
+          own = __builtin_amdgcn_alignbit(mask_word(a, node.mask, (from >> 5) + 1),
+                                          mask_word(a, node.mask, from >> 5), uint32_t(from) & 31);
+          if (there < 32) own &= (1u << max(there, 0)) - 1;
+          if (!node.alive) own = 0;
+        }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int32_t in = 16 * (i / 8) + 8 * int32_t(half) + i % 8, tok = at + 32 * u + in;
           if (nan >> in & 1) sc[u][i] = NAN;
-          if (tok < lo || tok >= hi || gone) sc[u][i] = -INFINITY;
+          if (((tok < lo || tok >= hi) && !(TREE && (own >> in & 1))) || gone) sc[u][i] = -INFINITY;
         }
       }
     }
@@ -897,7 +982,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 // wavefront takes all chunks' maxima and sums, a lane each, and 8 groups of
 // threads the chunks' O in turn, added up through LDS.  Bound by its own latency:
 // 3.7 us, whatever the number of chunks up to 64.
-template <int D, uint32_t COLS, uint32_t TILE>
+template <int D, uint32_t COLS, uint32_t TILE, bool TREE>
 __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   constexpr uint32_t kLanes = D / 4, kSub = 8;
   __shared__ __attribute__((aligned(16))) float4 lds[kSub][kLanes];
@@ -908,7 +993,7 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   if (int32_t(token) >= q.count) return;
   const uint32_t h = head / a.group, index = token * a.group + head % a.group;
   const uint32_t qt = index / COLS;
-  const Span sp = span_of<COLS, TILE>(a, q, qt * COLS);
+  const Span sp = span_of<COLS, TILE, TREE>(a, q, qt * COLS);
   if (sp.chunks <= 1) return;
   const uint64_t first =
       (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * COLS + index % COLS;
@@ -967,27 +1052,28 @@ size_t attn_bytes(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
   return p.chunks <= 1 ? 0 : part_cols(p, c, b) * (c->head_dim + 2) * sizeof(float);
 }
 
-template <int D>
+template <int D, bool TREE>
 void launch_attn(const AttnArgs &a, const Plan &p, bool pair, bool one_page, bool stream_codes,
                  dim3 grid, dim3 join, hipStream_t stream) {
   const dim3 block(256), join_block(2 * D);
   if (p.prompt) {
-    hipLaunchKernelGGL(prompt_kernel<D>, grid, block, 0, stream, a);
+    hipLaunchKernelGGL((prompt_kernel<D, TREE>), grid, block, 0, stream, a);
     if (p.chunks > 1)
-      hipLaunchKernelGGL((join_kernel<D, kPromptCols, kPromptTile>), join, join_block, 0, stream, a);
+      hipLaunchKernelGGL((join_kernel<D, kPromptCols, kPromptTile, TREE>), join, join_block, 0, stream,
+                         a);
     return;
   }
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
   auto pick = [&](auto one, auto streams) {
     constexpr bool ONE = decltype(one)::value, STREAM = decltype(streams)::value;
-    pair ? go(attn_kernel<D, ONE, STREAM, true>) : go(attn_kernel<D, ONE, STREAM, false>);
+    pair ? go(attn_kernel<D, ONE, STREAM, true, TREE>) : go(attn_kernel<D, ONE, STREAM, false, TREE>);
   };
   const std::true_type yes;
   const std::false_type no;
   if (one_page) stream_codes ? pick(yes, yes) : pick(yes, no);
   else stream_codes ? pick(no, yes) : pick(no, no);
   if (p.chunks > 1)
-    hipLaunchKernelGGL((join_kernel<D, kCols, kTile>), join, join_block, 0, stream, a);
+    hipLaunchKernelGGL((join_kernel<D, kCols, kTile, TREE>), join, join_block, 0, stream, a);
 }
 
 bool heads_ok(const eq_kv_cache *c, uint32_t q_heads) {
@@ -1002,10 +1088,7 @@ bool size_ok(const eq_kv_cache *c, const eq_kv_batch *b, uint32_t q_heads) {
   return uint64_t(c->kv_heads) * p.q_tiles * p.chunks <= kMaxBlocks;
 }
 
-}  // namespace
-
-extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
-                                              uint32_t q_heads) {
+size_t workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch, uint32_t q_heads) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || batch->n_seqs == 0 ||
       batch->max_new == 0 || !size_ok(cache, batch, q_heads))
     return 0;
@@ -1014,15 +1097,19 @@ extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq
                     cache, batch);
 }
 
-extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
-                           uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
-                           uint16_t *out, void *ws, size_t ws_bytes, hipStream_t stream) {
+template <bool TREE>
+int attention(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
+              uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
+              const uint32_t *mask, const int32_t *positions, uint16_t *out, void *ws,
+              size_t ws_bytes, hipStream_t stream) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || !(scale > 0.0f) || !std::isfinite(scale))
     return EQ_EINVAL;
+  if (TREE && batch->max_new > kMaxNodes) return EQ_EINVAL;
   if (batch->n_seqs == 0 || batch->max_new == 0) return EQ_OK;
   if (!q || !out || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15) ||
       q_stride % 8 || (batch->n_tokens > 1 && q_stride < uint64_t(q_heads) * cache->head_dim))
     return EQ_EINVAL;
+  if (TREE && (!mask || (window && !positions))) return EQ_EINVAL;
   const uint32_t group = q_heads / cache->kv_heads;
   if (!size_ok(cache, batch, q_heads)) return EQ_EINVAL;
   const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len,
@@ -1030,7 +1117,8 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
   const size_t need = attn_bytes(p, cache, batch);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return EQ_EINVAL;
   AttnArgs a{view(cache, batch), q, q_stride, out, static_cast<float *>(ws), nullptr, group, window,
-             p.q_tiles, p.chunks, p.chunk_tiles, scale * 1.44269504088896340736f};
+             p.q_tiles, p.chunks, p.chunk_tiles, scale * 1.44269504088896340736f, mask, positions,
+             (batch->max_new + 31) / 32};
   if (need)
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
   const dim3 grid(cache->kv_heads * p.q_tiles * p.chunks, batch->n_seqs);
@@ -1041,7 +1129,36 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
   const bool pair = pair_columns(batch->max_new, group);
   const bool stream_codes = stream_cache(p, batch->n_seqs, cache->kv_heads, cache->head_dim,
                                          batch->max_new, batch->max_len, window);
-  if (cache->head_dim == 128) launch_attn<128>(a, p, pair, one_page, stream_codes, grid, join, stream);
-  else launch_attn<64>(a, p, pair, one_page, stream_codes, grid, join, stream);
+  if (cache->head_dim == 128)
+    launch_attn<128, TREE>(a, p, pair, one_page, stream_codes, grid, join, stream);
+  else
+    launch_attn<64, TREE>(a, p, pair, one_page, stream_codes, grid, join, stream);
   return hipGetLastError() == hipSuccess ? EQ_OK : EQ_EHIP;
+}
+
+}  // namespace
+
+extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
+                                              uint32_t q_heads) {
+  return workspace_bytes(cache, batch, q_heads);
+}
+
+extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
+                           uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
+                           uint16_t *out, void *ws, size_t ws_bytes, hipStream_t stream) {
+  return attention<false>(cache, batch, q, q_stride, q_heads, scale, window, nullptr, nullptr, out, ws,
+                          ws_bytes, stream);
+}
+
+extern "C" size_t eq_attn_kv4_tree_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
+                                                   uint32_t q_heads) {
+  return batch && batch->max_new > kMaxNodes ? 0 : workspace_bytes(cache, batch, q_heads);
+}
+
+extern "C" int eq_attn_kv4_tree(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
+                                uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
+                                const uint32_t *mask, const int32_t *positions, uint16_t *out, void *ws,
+                                size_t ws_bytes, hipStream_t stream) {
+  return attention<true>(cache, batch, q, q_stride, q_heads, scale, window, mask, positions, out, ws,
+                         ws_bytes, stream);
 }

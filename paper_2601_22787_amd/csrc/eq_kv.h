@@ -10,6 +10,7 @@
 namespace eq_kv {
 
 constexpr uint32_t kUnit = 32;  // tokens that share a block of value codes
+constexpr uint32_t kMaxNodes = EQ_TREE_NODES;  // of a drafted tree
 // A launch has fewer than 2^32 threads along x: the most blocks of 256.
 constexpr uint32_t kMaxBlocks = (1u << 24) - 1;
 

@@ -440,6 +440,111 @@ __global__ __launch_bounds__(256) void read_kernel(View w, uint16_t *k, uint16_t
   }
 }
 
+// ----------------------------------------------------------------------- keep
+
+struct KeepArgs {
+  View w;  // (pages: of the first cache)
+  const int32_t *path, *kept;
+  int32_t *new_len;
+  uint8_t *pages[EQ_KEEP_CACHES];
+};
+
+// A wavefront takes a head of a sequence in one cache, and 8 aligned positions at a
+// time, the tokens of one dword of a channel's value codes.  What those become is read
+// before any of them is written, and what later positions become lies behind them:
+// the k-th node of a path is its sequence's k-th or a later one.
+template <int D>
+__global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
+  constexpr int N = D / 16;  // bytes of a token's key codes for each of 8 lanes
+  const View &w = a.w;
+  const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
+  const uint32_t s = blockIdx.y, h = blockIdx.x * 4 + wave;
+  uint8_t *const pages = a.pages[blockIdx.z];
+  const Seq q = sequence(w, s);
+  const int32_t kept = min(max(a.kept[s], 0), q.count);
+  if (a.new_len && blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0)
+    a.new_len[s] = q.count > 0 ? max(q.base, 0) + kept : max(w.kv_len[s], 0);
+  if (h >= w.kv_heads || kept <= 0) return;
+  const uint32_t t = lane >> 3, sub = lane & 7;
+  const uint32_t page_mask = (1u << w.page_shift) - 1;
+  const int32_t start = max(q.base, 0), end = min(q.base + kept, int32_t(w.max_len));
+  for (int32_t first = start & ~7; first < end; first += 8) {
+    const int32_t pos = first + int32_t(t), k = pos - q.base;
+    int32_t from = -1, src = -1, dst = -1;
+    if (pos >= start && pos < end) {
+      const int32_t node = a.path[q.row + k];
+      if (node > k && node < q.count) from = q.base + node;
+      if (from >= int32_t(w.max_len)) from = -1;
+    }
+    if (from >= 0) {
+      src = page_of(w, s, uint32_t(from));
+      dst = page_of(w, s, uint32_t(pos));
+    }
+    const bool on = src >= 0 && dst >= 0;
+    const uint64_t moving = __ballot(on);
+    if (!moving) continue;
+    const uint32_t slot = uint32_t(max(from, 0)) & page_mask, to = uint32_t(pos) & page_mask;
+    const uint64_t head = uint64_t(h) * w.head_bytes;
+    const uint8_t *const sp = pages + uint64_t(max(src, 0)) * w.page_bytes + head;
+    uint8_t *const dp = pages + uint64_t(max(dst, 0)) * w.page_bytes + head;
+    // keys: 8 lanes a token
+    uint32_t kc[N / 4];
+    uint8_t ks = 0, vs = 0;
+    auto ks_at = [&](uint32_t at) {
+      return w.ks_off + at / 16 * (D / 2) + (at % 4 * (D / 32) + sub) * 4 + at % 16 / 4;
+    };
+    if (on) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i)
+        kc[i] = reinterpret_cast<const uint32_t *>(sp + slot * (D / 2) + sub * N)[i];
+      if (sub < D / 32) ks = sp[ks_at(slot)];
+      if (sub == 7) vs = sp[w.vs_off + slot];
+    }
+    // values: two channels a lane, of all 8 tokens
+    const uint32_t pair = min(lane, uint32_t(D / 2 - 1));
+    uint32_t v[2] = {0, 0}, keep = ~0u;
+    uint8_t *out = nullptr;
+    uint32_t got[8][2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      got[j][0] = got[j][1] = 0;
+      if (!(moving >> (8 * j) & 1)) continue;
+      const uint32_t at = uint32_t(__shfl(int(slot), 8 * j));
+      const uint64_t page = uint64_t(uint32_t(__shfl(src, 8 * j))) * w.page_bytes;
+      const uint8_t *const p = pages + page + head + w.v_off + (at / 32 * D + 2 * pair) * 16 + at % 32 / 8 * 4;
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        got[j][c] = *reinterpret_cast<const uint32_t *>(p + 16 * c) >> (4 * (at % 8)) & 15;
+      if (!out)
+        out = pages + uint64_t(uint32_t(__shfl(dst, 8 * j))) * w.page_bytes + head + w.v_off +
+              ((uint32_t(first) & page_mask) / 32 * D + 2 * pair) * 16 + (uint32_t(first) & page_mask) % 32 / 8 * 4;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (!(moving >> (8 * j) & 1)) continue;
+      keep &= ~(15u << (4 * j));
+#pragma unroll
+      for (int c = 0; c < 2; ++c) v[c] |= got[j][c] << (4 * j);
+    }
+    uint32_t old[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) old[c] = *reinterpret_cast<const uint32_t *>(out + 16 * c);
+    __threadfence_block();  // all of it has been read
+    if (on) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i)
+        reinterpret_cast<uint32_t *>(dp + to * (D / 2) + sub * N)[i] = kc[i];
+      if (sub < D / 32) dp[ks_at(to)] = ks;
+      if (sub == 7) dp[w.vs_off + to] = vs;
+    }
+    if (lane < D / 2) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        *reinterpret_cast<uint32_t *>(out + 16 * c) = (old[c] & keep) | v[c];
+    }
+  }
+}
+
 // ----------------------------------------------------------------------- host
 
 bool rope_ok(const eq_rope *r, uint32_t head_dim) {
@@ -553,5 +658,34 @@ extern "C" int eq_kv_read(const eq_kv_cache *cache, const eq_kv_batch *batch, ui
   else
     hipLaunchKernelGGL((read_kernel<64>), grid, dim3(256), 0, stream, view(cache, batch), k, v,
                        units);
+  return done();
+}
+
+extern "C" int eq_kv_keep(const eq_kv_cache *const *caches, uint32_t n, const eq_kv_batch *batch,
+                          const int32_t *path, const int32_t *kept, int32_t *new_len,
+                          hipStream_t stream) {
+  if (!caches || n < 1 || n > EQ_KEEP_CACHES) return EQ_EINVAL;
+  for (uint32_t i = 0; i < n; ++i) {
+    const eq_kv_cache *const c = caches[i];
+    if (!batch_ok(c, batch) || c->page_tokens != caches[0]->page_tokens ||
+        c->kv_heads != caches[0]->kv_heads || c->head_dim != caches[0]->head_dim ||
+        c->n_pages != caches[0]->n_pages)
+      return EQ_EINVAL;
+    const uint64_t bytes = uint64_t(head_bytes(c->head_dim, c->page_tokens)) * c->kv_heads * c->n_pages;
+    for (uint32_t j = 0; j < i; ++j) {  // a page that is moved in twice
+      const uint8_t *const o = caches[j]->pages;
+      if (c->pages < o + bytes && o < c->pages + bytes) return EQ_EINVAL;
+    }
+  }
+  if (batch->max_new > kMaxNodes) return EQ_EINVAL;
+  if (batch->n_seqs == 0) return EQ_OK;
+  if (!kept || (batch->max_new && !path) || new_len == batch->kv_len) return EQ_EINVAL;
+  KeepArgs a{view(caches[0], batch), path, kept, new_len, {}};
+  for (uint32_t i = 0; i < n; ++i) a.pages[i] = caches[i]->pages;
+  const dim3 grid((caches[0]->kv_heads + 3) / 4, batch->n_seqs, n);
+  if (caches[0]->head_dim == 128)
+    hipLaunchKernelGGL((keep_kernel<128>), grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((keep_kernel<64>), grid, dim3(256), 0, stream, a);
   return done();
 }
