@@ -462,8 +462,9 @@ size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, 
  * replacement loses x and is normalised, and the next is tested.  (Without a draft: x
  * is accepted where random < p(x), else p loses x.)  The accepted child is next.  Where
  * none is, the token behind the path is the first at which the running sum of what is
- * left of p, in the tokens' order, passes random[row of node 0] times the whole (of
- * p itself, where nothing is left).  random: fp32, taken into [0, 1 - 2^-24] (NaN: 0).
+ * left of p, in the tokens' order, passes random[row of node 0] times the whole.  Where
+ * less than 2^-32 of p is left, no further child is tested and that token is of p
+ * itself.  random: fp32, taken into [0, 1 - 2^-24] (NaN: 0).
  * A temperature that is not above 0: the child that is the target's largest logit is
  * accepted, the lowest of equal ones; random and draft are not looked at.
  * path: the kept nodes of each sequence from its first row on, node 0 first, then -1;
@@ -472,7 +473,7 @@ size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, 
  * nothing above -infinity (the path up to there is kept).  Tokens outside the
  * vocabulary are never accepted, nor nodes that are not their parent's later rows.
  * All in 64 bits: tokens are those of exact arithmetic but where a random number is
- * within about 2^-45 of a border.  max_children bounds a node's children (1: a
+ * within about 2^-36 of a border.  max_children bounds a node's children (1: a
  * chain); with more than that, results are the same, and slower.  vocab is at most
  * 2^24.  ws/ws_bytes: at least eq_tree_verify_workspace_bytes(), 16-byte aligned;
  * nothing in it is kept between calls. */

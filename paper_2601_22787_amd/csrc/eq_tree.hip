@@ -18,12 +18,15 @@
 // instructions issue at the rate of 32-bit ones here, and an exponential is 20.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "eq.h"
 #include "eq_device.h"
 
 namespace {
+
+typedef int int2v __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t kMaxNodes = EQ_TREE_NODES;
 constexpr uint32_t kChunk = 1024;  // logits a wavefront takes at a time
@@ -40,7 +43,8 @@ struct BatchArgs {
 };
 
 __device__ inline Rows rows_of(const BatchArgs &b, uint32_t s) {
-  const int32_t row = b.seq_start[s], end = b.seq_start[s + 1];
+  const int32_t row = int32_t(eq_dev::as_const(b.seq_start)[s]);
+  const int32_t end = int32_t(eq_dev::as_const(b.seq_start)[s + 1]);
   Rows r{row, 0, 0};
   if (row < 0 || end <= row || uint32_t(row) >= b.n_tokens) return r;
   r.n = end - row;
@@ -94,13 +98,34 @@ __global__ __launch_bounds__(kMaxNodes) void tree_mask_kernel(MaskArgs a) {
 
 // -------------------------------------------------------------- verification
 
-// A chunk's largest logit, where it first is (-1: the chunk holds a NaN or +infinity),
-// and the sum of exp((x - max) / T).
+// Of a chunk or a few: the sum of exp((x - max) / T), max being the largest logit or one
+// near it (at temperature 0 the largest, and no sum); the first place of the largest (at
+// temperature 0, else any), -1 where there is a NaN or +infinity.
 struct Part {
   double sum;
   float max;
   int32_t arg;
 };
+
+// A row's distribution: exp((x - max) / T) inv, with max as above; best: its first largest
+// logit (at temperature 0, else any token), or -1 where the row has no distribution.
+struct Stat {
+  double inv;
+  float max;
+  int32_t best;
+};
+
+// Where a sequence's walk stands: at node `cur`, whose children before `child` have been
+// rejected.
+struct State {
+  double t, mass, left;  // mass: G(t), or what the rejected points have left of p
+  uint32_t cur, child, kept;
+  uint32_t waits;        // for the sums of max(p - t q, 0)
+};
+
+constexpr double kLeast = 0x1p-32;  // of p: less is taken for nothing
+constexpr uint32_t kRounds = 4;
+constexpr uint32_t kStatWaves = 6144, kMostPer = 3;
 
 struct VerifyArgs {
   BatchArgs b;
@@ -109,33 +134,72 @@ struct VerifyArgs {
   uint64_t target_stride, draft_stride;
   const float *temperature, *random;
   int32_t *path, *kept, *next;
-  Part *target_part, *draft_part;  // [n_tokens][chunks]
-  double *sums;                    // [n_seqs][chunks]
-  uint32_t vocab, chunks;
+  // workspace
+  Part *part;                      // [n_tokens][chunks], of the target's rows
+  Part *target_group, *draft_group;  // [n_tokens][groups], `per` chunks of 4 wavefronts each
+  double *sums[2];                 // [n_seqs][chunks], of even and odd passes
+  double *px, *qx;                 // [n_tokens]
+  Stat *target_stat, *draft_stat;  // [n_tokens]
+  State *state[2];                 // [n_seqs], behind even and odd passes
+  uint32_t vocab, chunks, per, groups;
   bool replace;
 };
 
-// exp(x) for x <= 0, 0 where it is below 2^-1022 (and for NaN): x = k ln 2 + r, the
-// series of exp(r) to its 12th power (|r| <= ln 2 / 2: the next term is 2^-52).
-__device__ inline double exp_down(double x) {
-  x = fmax(x, -800.0);
-  const double k = __builtin_rint(x * 1.4426950408889634074);
-  double r = __builtin_fma(k, -2977044471.0 / 4294967296.0, x);  // ln 2: its first 32 bits,
-  r = __builtin_fma(k, -1.9082149292705877e-10, r);          // and the rest
-  double y = 1.0 / 479001600.0;
-  y = __builtin_fma(y, r, 1.0 / 39916800.0);
-  y = __builtin_fma(y, r, 1.0 / 3628800.0);
-  y = __builtin_fma(y, r, 1.0 / 362880.0);
-  y = __builtin_fma(y, r, 1.0 / 40320.0);
-  y = __builtin_fma(y, r, 1.0 / 5040.0);
-  y = __builtin_fma(y, r, 1.0 / 720.0);
-  y = __builtin_fma(y, r, 1.0 / 120.0);
-  y = __builtin_fma(y, r, 1.0 / 24.0);
-  y = __builtin_fma(y, r, 1.0 / 6.0);
-  y = __builtin_fma(y, r, 0.5);
-  y = __builtin_fma(y, r, 1.0);
-  y = __builtin_fma(y, r, 1.0);
-  return __builtin_ldexp(y, int(k));
+// 2^f for |f| <= 1/2: the polynomial that meets it at 0 and at the 8 Chebyshev points,
+// 2^-38.8 relative.
+__device__ inline double exp2_near(double f) {
+  double z = 1.325080551750225e-06;
+  z = __builtin_fma(z, f, 1.5303700711365693e-05);
+  z = __builtin_fma(z, f, 0.00015403475186530786);
+  z = __builtin_fma(z, f, 0.0013333478473685416);
+  z = __builtin_fma(z, f, 0.00961812913523614);
+  z = __builtin_fma(z, f, 0.055504109063258665);
+  z = __builtin_fma(z, f, 0.24022650695888503);
+  z = __builtin_fma(z, f, 0.6931471805568324);
+  return __builtin_fma(z, f, 1.0);
+}
+
+// exp(d / T) for d up to 0 or not far above, c = log2 e / T; 0 far down (and for -infinity, also times 0, and
+// NaN).
+__device__ inline double exp_down(double d, double c) {
+  const double y = fmax(d * c, -1100.0), z = y + 0x1.8p52;  // y rounded, in the low bits
+  return __builtin_ldexp(exp2_near(y - (z - 0x1.8p52)), int(__builtin_bit_cast(uint64_t, z)));
+}
+
+// exp((x - ref) / T) of logits near ref, but for a common factor, `shift`: in 13 64-bit
+// instructions and an integer one, where exp_down has 17.  With K = ref c rounded, adding
+// 3 2^51 - K to x c leaves it rounded, with the exponent that is wanted in the low bits.
+// For x in [low, high], where that exponent stays in range; fast: ref c is not so large
+// that its own rounding would show.
+struct Power {
+  double c, add, shift;  // shift: 2^(K - ref c)
+  float ref, low, high;
+  bool fast;
+  __device__ inline Power(float r, double per_temp, double temp) : c(per_temp), ref(r) {
+    const double top = double(r) * c, k = __builtin_rint(top), far = 0.6931471805599453 * temp;
+    fast = c >= 0x1p-100 && fabs(top) <= 4096.0;
+    add = 0x1.8p52 - k;
+    shift = fast ? exp2_near(-__builtin_fma(double(r), c, -k)) : 1.0;
+    low = fast ? float((k - 900.0) * far) : INFINITY;
+    high = fast ? float((k + 500.0) * far) : NAN;  // (nothing is below that)
+  }
+  __device__ inline double operator()(float x) const {
+    const double d = double(x), z = __builtin_fma(d, c, add);
+    const double y = exp2_near(__builtin_fma(d, c, -(z - add)));
+    int2v u = __builtin_bit_cast(int2v, y);
+    u[1] += __builtin_bit_cast(int2v, z)[0] << 20;
+    return __builtin_bit_cast(double, u);
+  }
+};
+
+// The next N of 16 values to the front.  Loops over a few at a time stay loops by it:
+// unrolled, the exponentials of a chunk are 10 KB of code that a wavefront runs through
+// once, and fetching that took longer than the rest (128 chunks of 32 rows, two logits
+// each: 21 us, as a loop 8).
+template <int N>
+__device__ inline void next(float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16 - N; ++i) x[i] = x[i + N];
 }
 
 template <typename T>
@@ -144,393 +208,727 @@ __device__ inline float logit(const T *row, uint32_t i) {
   else return eq_dev::bf16_to_f32(row[i]);
 }
 
-// A lane's 16 logits of a chunk, four in a row: element 4 i + e is number 256 i + 4
-// lane + e.  -infinity behind the vocabulary.  Rows start at any element.
+// A lane's 16 logits of a chunk: element 4 i + e is number 256 i + 4 lane + e.  Rows
+// start at any element.  In two parts, so that loads stay in flight: what was loaded,
+// and its values.  (A load under a condition would be waited for where the branches
+// meet.)
 template <typename T>
-__device__ inline void load_chunk(const T *row, uint32_t vocab, uint32_t first, uint32_t lane,
-                                  float (&x)[16]) {
+struct Raw {
+  T v[4][4];
+};
+template <typename T>
+__device__ inline Raw<T> load_full(const T *row, uint32_t chunk, uint32_t lane) {
+  Raw<T> r;
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i) {
-    const uint32_t at = first + 256 * i + 4 * lane;
-    if (at + 4 <= vocab) {
-      T v[4];
-      __builtin_memcpy(v, row + at, sizeof(v));
+  for (uint32_t i = 0; i < 4; ++i)
+    __builtin_memcpy(r.v[i], row + chunk * kChunk + 256 * i + 4 * lane, sizeof(r.v[i]));
+  return r;
+}
+template <typename T>
+__device__ inline void values(const Raw<T> &r, float (&x)[16]) {
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) x[4 * i + e] = logit(v, e);
-    } else {
+  for (uint32_t i = 0; i < 16; ++i) x[i] = logit(r.v[i / 4], i % 4);
+}
+// The last chunk, -infinity behind the vocabulary.
+template <typename T>
+__device__ inline void load_rest(const T *row, uint32_t vocab, uint32_t chunk, uint32_t lane,
+                                 float (&x)[16]) {
 #pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) x[4 * i + e] = at + e < vocab ? logit(row, at + e) : -INFINITY;
-    }
+  for (uint32_t i = 0; i < 16; ++i) {
+    const uint32_t at = chunk * kChunk + 256 * (i / 4) + 4 * lane + i % 4;
+    const float v = logit(row, min(at, vocab - 1));
+    x[i] = at < vocab ? v : -INFINITY;
   }
 }
 
-__device__ inline double wave_sum64(double v) {
+// 16 logits in a row, -infinity behind the vocabulary.
+template <typename T>
+__device__ inline void load_run(const T *row, uint32_t vocab, uint32_t at, float (&x)[16]) {
+  if (at + 16 <= vocab) {
+    T v[16];
+    __builtin_memcpy(v, row + at, sizeof(v));
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    for (uint32_t e = 0; e < 16; ++e) x[e] = logit(v, e);
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < 16; ++e) x[e] = at + e < vocab ? logit(row, at + e) : -INFINITY;
+  }
+}
+
+// v of the lane that CTRL names, `none` where there is none or the row is not in ROWS.
+template <int CTRL, int ROWS>
+__device__ inline float from_lane(float v, float none) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL,
+                                                    ROWS, 0xF, false));
+}
+template <int CTRL, int ROWS>
+__device__ inline double from_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(u)), CTRL, ROWS, 0xF, true));
+  const uint32_t hi = uint32_t(__builtin_amdgcn_update_dpp(0, int(uint32_t(u >> 32)), CTRL, ROWS, 0xF, true));
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ inline double lane_value(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(u)), lane));
+  const uint32_t hi = uint32_t(__builtin_amdgcn_readlane(int(uint32_t(u >> 32)), lane));
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+
+// Sums of the lanes up to each: within rows of 16, then from row to row.
+__device__ inline double wave_scan(double v) {
+  v += from_lane<0x111, 0xF>(v);
+  v += from_lane<0x112, 0xF>(v);
+  v += from_lane<0x114, 0xF>(v);
+  v += from_lane<0x118, 0xF>(v);
+  v += from_lane<0x142, 0xA>(v);  // row_bcast:15
+  v += from_lane<0x143, 0xC>(v);  // row_bcast:31
   return v;
+}
+__device__ inline double wave_sum(double v) { return lane_value(wave_scan(v), 63); }
+
+__device__ inline float wave_max(float v) {
+  v = fmaxf(v, from_lane<0x111, 0xF>(v, -INFINITY));
+  v = fmaxf(v, from_lane<0x112, 0xF>(v, -INFINITY));
+  v = fmaxf(v, from_lane<0x114, 0xF>(v, -INFINITY));
+  v = fmaxf(v, from_lane<0x118, 0xF>(v, -INFINITY));
+  v = fmaxf(v, from_lane<0x142, 0xA>(v, -INFINITY));
+  v = fmaxf(v, from_lane<0x143, 0xC>(v, -INFINITY));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 __device__ inline float temperature_of(const VerifyArgs &a, uint32_t s) {
-  return a.temperature ? a.temperature[s] : 1.0f;
+  return a.temperature ? __uint_as_float(eq_dev::as_const(a.temperature)[s]) : 1.0f;
+}
+__device__ inline double per_temperature(float temp) {
+  return temp > 0.0f ? 1.4426950408889634 / double(temp) : 0.0;
 }
 
-// The statistics of a row's chunks, a wavefront each.  Draft rows of nodes without
-// children are left out.
+// A chunk's first largest logit.
+__device__ inline Part largest(const float (&x)[16], uint32_t chunk, float top) {
+  bool bad = false;
+  int32_t arg = -1;
+#pragma unroll
+  for (int i = 3; i >= 0; --i) {
+    uint32_t mine = 4;  // the first of four that is the largest
+#pragma unroll
+    for (int e = 3; e >= 0; --e) {
+      bad = bad || !(x[4 * i + e] < INFINITY);
+      mine = x[4 * i + e] == top ? e : mine;
+    }
+    const uint64_t m = __ballot(mine < 4);
+    if (m) {
+      const int l = __ffsll((unsigned long long)m) - 1;
+      arg = int32_t(chunk * kChunk) + 256 * i + 4 * l + __builtin_amdgcn_readlane(int(mine), l);
+    }
+  }
+  return Part{0.0, top, __any(bad) ? -1 : arg};
+}
+
+// The statistics of a row's chunks, `per` of them for a wavefront, one's loads in flight
+// beside another's exponentials, and of the block's chunks together.  Draft rows of nodes
+// without children are left out.
+//
+// A wavefront's first chunk sets the reference of its exponentials, and others keep it
+// while they are near: a chunk then has no maximum to agree on first.  A NaN comes out in
+// the sum.  Chunks with far or infinite logits take exp_down.
+template <typename T>
+__device__ __forceinline__ void row_stats(const T *row, uint32_t vocab, uint32_t chunk, uint32_t end,
+                                          uint32_t lane, float temp, double per_temp, Part *out) {
+  const uint32_t full = min(end, vocab / kChunk);  // behind those, one at most
+  const bool greedy = !(temp > 0.0f);
+  Raw<T> raw;
+  if (chunk < full) raw = load_full(row, chunk, lane);
+  Power power(INFINITY, per_temp, double(temp));  // (near nothing)
+#pragma unroll 1
+  for (; chunk < end; ++chunk, ++out) {
+    float x[16];
+    if (chunk < full) {
+      values(raw, x);
+      raw = load_full(row, min(chunk + 1, full - 1), lane);
+    } else {
+      load_rest(row, vocab, chunk, lane, x);
+    }
+    float high = x[0], low = x[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) high = fmaxf(high, x[e]), low = fminf(low, x[e]);
+    if (greedy) {
+      const Part p = largest(x, chunk, wave_max(high));
+      if (lane == 0) *out = p;
+      continue;
+    }
+    if (!__all(high <= power.high)) power = Power(wave_max(high), per_temp, double(temp));
+    double sum = 0.0;
+    bool bad = false;
+    if (power.fast && __all(low >= power.low)) {
+#pragma unroll 1
+      for (int i = 0; i < 16; i += 8, next<8>(x)) {
+#pragma unroll
+        for (int h = 0; h < 8; h += 4) {
+          sum += (power(x[h]) + power(x[h + 1])) + (power(x[h + 2]) + power(x[h + 3]));
+          __builtin_amdgcn_sched_barrier(0);  // (eight side by side would take 130 registers)
+        }
+      }
+      sum = wave_sum(sum) * power.shift;
+      bad = sum != sum;
+    } else if (power.ref > -INFINITY) {
+#pragma unroll 1
+      for (int i = 0; i < 16; i += 4, next<4>(x)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          bad = bad || !(x[e] < INFINITY);
+          sum += exp_down(double(x[e]) - double(power.ref), per_temp);
+        }
+      }
+      sum = wave_sum(sum);
+      bad = __any(bad);
+    }
+    if (lane == 0) *out = Part{sum, power.ref, bad ? -1 : int32_t(chunk * kChunk)};
+  }
+}
+
+// Statistics of parts, a lane's each, in all lanes: the largest, its first place, and the
+// sum of exp((x - max) / T).
+__device__ inline Part join_lanes(Part p, bool on, double per_temp) {
+  const bool bad = __any(on && p.arg < 0);
+  const float top = wave_max(on ? p.max : -INFINITY);
+  const uint64_t m = __ballot(on && p.max == top);
+  const int32_t arg = m ? __builtin_amdgcn_readlane(p.arg, __ffsll((unsigned long long)m) - 1) : -1;
+  const double sum = on && p.max > -INFINITY ? p.sum * exp_down(double(p.max) - double(top), per_temp) : 0.0;
+  return Part{wave_sum(sum), top, bad ? -1 : arg};
+}
+
 template <typename TT, typename TD>
 __global__ __launch_bounds__(256) void row_stats_kernel(VerifyArgs a) {
+  __shared__ Part parts[4 * kMostPer];
   const uint32_t s = blockIdx.z, i = blockIdx.y;
-  const uint32_t groups = (a.chunks + 3) / 4;
-  const bool drafted = blockIdx.x >= groups;
+  const bool drafted = blockIdx.x >= a.groups;
   const Rows r = rows_of(a.b, s);
   if (int32_t(i) >= r.count) return;
   const float temp = temperature_of(a, s);
-  const bool greedy = !(temp > 0.0f);
   if (drafted) {
-    if (greedy) return;
+    if (!(temp > 0.0f)) return;
     const int32_t j = int32_t(threadIdx.x);
     if (!__syncthreads_or(j > int32_t(i) && j < r.count && a.parents[r.row + j] == int32_t(i))) return;
   }
   const uint32_t lane = threadIdx.x & 63, wave = eq_dev::uniform(threadIdx.x >> 6);
-  const uint32_t chunk = (blockIdx.x - (drafted ? groups : 0)) * 4 + wave;
-  if (chunk >= a.chunks) return;
+  const uint32_t group = blockIdx.x - (drafted ? a.groups : 0), first = group * 4 * a.per;
+  const uint32_t chunk = first + wave * a.per, end = min(chunk + a.per, a.chunks);
   const uint64_t row = uint64_t(r.row) + i;
-  float x[16];
-  if (drafted)
-    load_chunk(static_cast<const TD *>(a.draft) + row * a.draft_stride, a.vocab, chunk * kChunk, lane, x);
+  const double per_temp = per_temperature(temp);
+  Part *const out = parts + wave * a.per;
+  const TT *const target = static_cast<const TT *>(a.target) + row * a.target_stride;
+  const TD *const draft = static_cast<const TD *>(a.draft) + row * a.draft_stride;
+  if constexpr (std::is_same<TT, TD>::value)
+    row_stats(drafted ? draft : target, a.vocab, chunk, end, lane, temp, per_temp, out);
+  else if (drafted)
+    row_stats(draft, a.vocab, chunk, end, lane, temp, per_temp, out);
   else
-    load_chunk(static_cast<const TT *>(a.target) + row * a.target_stride, a.vocab, chunk * kChunk, lane,
-               x);
-  float top = x[0];
-  bool bad = false;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    top = fmaxf(top, x[e]);
-    bad = bad || !(x[e] < INFINITY);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  int32_t arg = 0x7FFFFFFF;
-#pragma unroll
-  for (int e = 15; e >= 0; --e)
-    if (x[e] == top) arg = int32_t(chunk * kChunk + 256 * (e / 4) + 4 * lane + e % 4);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) arg = min(arg, __shfl_xor(arg, d));
-  double sum = 0.0;
-  if (!greedy && top > -INFINITY) {
-    const double inv = 1.0 / double(temp), m = double(top);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) sum += exp_down((double(x[e]) - m) * inv);
-    sum = wave_sum64(sum);
-  }
-  if (__any(bad)) arg = -1;
-  if (lane == 0) (drafted ? a.draft_part : a.target_part)[row * a.chunks + chunk] = Part{sum, top, arg};
+    row_stats(target, a.vocab, chunk, end, lane, temp, per_temp, out);
+  __syncthreads();
+  if (wave) return;
+  const bool on = lane < min(4 * a.per, a.chunks - first);
+  const Part p = parts[on ? lane : 0];
+  if (!drafted && on) a.part[row * a.chunks + first + lane] = p;
+  const Part all = join_lanes(p, on, per_temp);
+  if (lane == 0) (drafted ? a.draft_group : a.target_group)[row * a.groups + group] = all;
 }
 
-// A row's distribution: exp((x - max) / T) inv; best: its first largest logit, or -1
-// where the row has no distribution.
-struct Stat {
-  double inv;
-  float max;
-  int32_t best;
-};
-
-// A row's statistics from its chunks', by 16 lanes: the same in all of them.
-__device__ inline Stat join_parts(const Part *part, uint32_t chunks, uint32_t lane16, double inv_temp) {
+// A row's statistics from its groups', by `lanes` neighbouring lanes: the same in all.
+__device__ inline Stat join_groups(const Part *part, uint32_t groups, uint32_t lane, uint32_t lanes,
+                                   double per_temp) {
   float top = -INFINITY;
   int32_t arg = 0x7FFFFFFF;
   bool bad = false;
-  for (uint32_t c = lane16; c < chunks; c += 16) {
-    const Part p = part[c];
-    bad = bad || p.arg < 0;
-    if (p.max > top || arg == 0x7FFFFFFF) top = p.max, arg = p.arg;
-  }
-#pragma unroll
-  for (int d = 1; d < 16; d *= 2) {
-    const float m = __shfl_xor(top, d);
-    const int32_t j = __shfl_xor(arg, d);
-    const int b = __shfl_xor(int(bad), d);
-    bad = bad || b;
-    if (m > top || (m == top && j < arg)) top = m, arg = j;
-  }
   double sum = 0.0;
-  for (uint32_t c = lane16; c < chunks; c += 16) {
-    const Part p = part[c];
-    sum += p.max > -INFINITY ? p.sum * exp_down((double(p.max) - double(top)) * inv_temp) : 0.0;
-  }
+#pragma unroll 1
+  for (uint32_t c0 = 0; c0 < groups; c0 += 8 * lanes) {
+    Part p[8];
 #pragma unroll
-  for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
-  return Stat{1.0 / sum, top, bad || top == -INFINITY ? -1 : arg};
+    for (uint32_t j = 0; j < 8; ++j) p[j] = part[min(c0 + lanes * j + lane, groups - 1)];
+    float high = top;
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j) {
+      bad = bad || p[j].arg < 0;
+      if (p[j].max > high || arg == 0x7FFFFFFF) high = p[j].max, arg = p[j].arg;
+    }
+    if (high > -INFINITY) {
+      sum *= exp_down(double(top) - double(high), per_temp);
+#pragma unroll 1
+      for (uint32_t c = c0 + lane; c < min(groups, c0 + 8 * lanes); c += lanes) {
+        sum += p[0].sum * exp_down(double(p[0].max) - double(high), per_temp);
+#pragma unroll
+        for (uint32_t j = 0; j < 7; ++j) p[j].sum = p[j + 1].sum, p[j].max = p[j + 1].max;
+      }
+    }
+    top = high;
+  }
+  float all = top;
+#pragma unroll 1
+  for (uint32_t d = 1; d < lanes; d *= 2) {
+    const float m = __shfl_xor(all, int(d));
+    const int32_t j = __shfl_xor(arg, int(d)), b = __shfl_xor(int(bad), int(d));
+    bad = bad || b;
+    if (m > all || (m == all && j < arg)) all = m, arg = j;
+  }
+  sum = top > -INFINITY ? sum * exp_down(double(top) - double(all), per_temp) : 0.0;
+#pragma unroll 1
+  for (uint32_t d = 1; d < lanes; d *= 2) sum += __shfl_xor(sum, int(d));
+  return Stat{1.0 / sum, all, bad || all == -INFINITY ? -1 : arg};
 }
 
-// One block walks a sequence's tree.  Every wavefront takes the same decisions.
+// A node's place among the others.
+struct Link {
+  uint16_t first, next;  // its first child, the next child of its parent; kNone
+  uint32_t again;        // an earlier child of its parent has the same token
+};
+constexpr uint32_t kNone = 0xFFFF;
+
+struct Node {
+  int32_t up, token;  // up: -2 for what hangs on nothing
+  float random;
+};
+
+// What a block holds of a sequence's tree.
+struct Tree {
+  Stat target[kMaxNodes], draft[kMaxNodes];
+  double px[kMaxNodes], qx[kMaxNodes];  // p and q of a node's token at its parent
+  float random[kMaxNodes];
+  int32_t up[kMaxNodes], token[kMaxNodes];
+  Link link[kMaxNodes];
+  uint32_t hidden[kChunk / 32];
+  double weight[16][64];  // of a chunk's tokens, 16 a lane; or the chunks' sums
+  __device__ inline void put(uint32_t i, const Node &n) {
+    up[i] = n.up, token[i] = n.token, random[i] = n.random;
+    link[i] = Link{kNone, kNone, 0};
+  }
+};
+constexpr uint32_t kLocalChunks = 1024;  // sums that `weight` has room for
+
+// A sequence's node; behind the last one, none.
+__device__ inline Node load_node(const VerifyArgs &a, const Rows &r, uint32_t i) {
+  const bool on = int32_t(i) < r.count;
+  const int32_t row = r.row + int32_t(on ? i : 0);
+  const int32_t p = a.parents[row];
+  return Node{on && i > 0 && p >= 0 && p < int32_t(i) ? p : -2, a.tokens[row], a.random[row]};
+}
+
+// The nodes' links, a thread each: a node looks through the later ones, four at a time.
+__device__ inline void link_tree(Tree &tree, uint32_t count, uint32_t tid) {
+  if (tid >= count) return;
+  const int32_t up = tree.up[tid], token = tree.token[tid];
+  uint32_t first = kNone, next = kNone;
+#pragma unroll 1
+  for (uint32_t j0 = (tid + 1) / 4 * 4; j0 < count; j0 += 4) {
+    const int4 u = *reinterpret_cast<const int4 *>(tree.up + j0);
+    const int4 k = *reinterpret_cast<const int4 *>(tree.token + j0);
+    const int32_t us[4] = {u.x, u.y, u.z, u.w}, ks[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e) {
+      const uint32_t j = j0 + e;
+      if (us[e] == int32_t(tid)) first = min(first, j);
+      if (j > tid && us[e] == up && up >= 0) {
+        next = min(next, j);
+        if (ks[e] == token) tree.link[j].again = 1;
+      }
+    }
+  }
+  tree.link[tid].first = uint16_t(first), tree.link[tid].next = uint16_t(next);
+}
+
+// A wavefront's walk through a tree.
 template <typename TT, typename TD, bool POINTS>
-__global__ __launch_bounds__(1024) void walk_kernel(VerifyArgs a) {
-  __shared__ Stat target_stat[kMaxNodes], draft_stat[kMaxNodes];
-  __shared__ double px[kMaxNodes], qx[kMaxNodes];  // p and q of a node's token at its parent
-  __shared__ int32_t up[kMaxNodes], token[kMaxNodes];
-  __shared__ uint32_t inner[kMaxNodes], hidden[kChunk / 32];
-  const uint32_t s = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const uint32_t wave = eq_dev::uniform(tid >> 6), waves = blockDim.x >> 6;
-  const Rows r = rows_of(a.b, s);
-  if (r.count <= 0) {
-    if (tid == 0) a.kept[s] = 0, a.next[s] = -1;
-    return;
+struct Walk {
+  const VerifyArgs &a;
+  Tree &tree;
+  Rows r;
+  uint32_t s, count, lane;
+  bool greedy, writes;  // writes: the one of a sequence's blocks that does
+  double per_temp;
+  double *sums;
+  State st;
+
+  __device__ inline Walk(const VerifyArgs &args, Tree &t, uint32_t seq, const Rows &rows, bool writer,
+                         double *chunk_sums)
+      : a(args), tree(t), r(rows), s(seq), count(uint32_t(rows.count)), lane(threadIdx.x & 63),
+        writes(writer), sums(chunk_sums + uint64_t(seq) * args.chunks) {
+    const float temp = temperature_of(a, s);
+    greedy = !(temp > 0.0f);
+    per_temp = per_temperature(temp);
   }
-  const uint32_t count = uint32_t(r.count);
-  const float temp = temperature_of(a, s);
-  const bool greedy = !(temp > 0.0f);
-  const double inv_temp = greedy ? 1.0 : 1.0 / double(temp);
-  auto target_row = [&](uint32_t i) {
+
+  __device__ inline const TT *target_row(uint32_t i) const {
     return static_cast<const TT *>(a.target) + (uint64_t(r.row) + i) * a.target_stride;
-  };
-  auto draft_row = [&](uint32_t i) {
+  }
+  __device__ inline const TD *draft_row(uint32_t i) const {
     return static_cast<const TD *>(a.draft) + (uint64_t(r.row) + i) * a.draft_stride;
-  };
-
-  if (tid < count) {
-    const int32_t p = a.parents[r.row + int32_t(tid)];
-    up[tid] = tid > 0 && p >= 0 && p < int32_t(tid) ? p : -1;
-    token[tid] = a.tokens[r.row + int32_t(tid)];
-    inner[tid] = 0;
   }
-  __syncthreads();
-  if (tid < count && up[tid] >= 0) inner[up[tid]] = 1;
-  __syncthreads();
-  for (uint32_t k = tid / 16; k < (POINTS ? 1 : 2) * count; k += blockDim.x / 16) {
-    const bool drafted = k >= count;
-    const uint32_t i = drafted ? k - count : k;
-    if (drafted && (greedy || !inner[i])) continue;
-    const Stat st = join_parts((drafted ? a.draft_part : a.target_part) + (uint64_t(r.row) + i) * a.chunks,
-                               a.chunks, tid & 15, inv_temp);
-    if ((tid & 15) == 0) (drafted ? draft_stat : target_stat)[i] = st;
+  __device__ inline double prob(const Stat &v, float x) const {
+    return exp_down(double(x) - double(v.max), per_temp) * v.inv;
   }
-  __syncthreads();
-  auto prob = [&](const Stat &st, float x) {
-    return exp_down((double(x) - double(st.max)) * inv_temp) * st.inv;
-  };
-  if (tid < count && up[tid] >= 0 && uint32_t(token[tid]) < a.vocab && !greedy) {
-    const uint32_t p = uint32_t(up[tid]), x = uint32_t(token[tid]);
-    px[tid] = prob(target_stat[p], logit(target_row(p), x));
-    if constexpr (POINTS) qx[tid] = 1.0;
-    else qx[tid] = prob(draft_stat[p], logit(draft_row(p), x));
+  __device__ inline double random_of(uint32_t i) const {
+    return double(fminf(fmaxf(tree.random[i], 0.0f), 0.99999994f));  // (NaN: 0)
   }
-  __syncthreads();
+  __device__ inline bool outside(uint32_t i) const { return uint32_t(tree.token[i]) >= a.vocab; }
 
-  auto random_of = [&](uint32_t i) {
-    const float u = a.random[r.row + int32_t(i)];
-    return double(fminf(fmaxf(u, 0.0f), 0.99999994f));  // (NaN: 0)
-  };
-  // the node's next child behind node `last`, or `count`
-  auto child = [&](uint32_t node, uint32_t last) {
-    for (uint32_t c = (last + 1) / 64 * 64; c < count; c += 64) {
-      const uint32_t j = c + lane;
-      const uint64_t m = __ballot(j > last && j < count && up[j] == int32_t(node));
-      if (m) return c + uint32_t(__ffsll((unsigned long long)m)) - 1;
-    }
-    return count;
-  };
+  __device__ inline void stand_at(uint32_t node) {
+    st.cur = node, st.child = tree.link[node].first;
+    st.t = 0.0, st.mass = 1.0, st.left = 1.0;
+  }
+  __device__ inline void go_down(uint32_t c) {
+    if (writes && lane == 0) a.path[r.row + int32_t(st.kept)] = int32_t(c);
+    ++st.kept;
+    stand_at(c);
+  }
 
-  uint32_t cur = 0, last = 0, kept = 1;
-  double t = 0.0, mass = 1.0, left = 1.0;
-  if (tid == 0) a.path[r.row] = 0;
-  int32_t next = -1;
-  double *const sums = a.sums + uint64_t(s) * a.chunks;
-  const uint32_t chunks = a.chunks;
-  // weights of a chunk at the node where the walk stands; POINTS: without the tokens
-  // in `hidden`, where any are
-  auto weights = [&](uint32_t chunk, double tt, bool cut, double (&w)[16]) {
-    float x[16];
-    load_chunk(target_row(cur), a.vocab, chunk * kChunk, lane, x);
-    const Stat ps = target_stat[cur];
+  // The weights max(p - t q, 0) of 16 tokens, four at a time: put(i, w).
+  template <typename F>
+  __device__ inline void weights(float (&p)[16], float (&q)[16], F &&put) const {
+    const Stat ps = tree.target[st.cur], qs = POINTS ? ps : tree.draft[st.cur];
+    const bool less = !POINTS && st.t > 0.0;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i, next<4>(p), next<4>(q)) {
+      double w[4];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) w[e] = prob(ps, x[e]);
-    if constexpr (!POINTS) {
-      if (tt > 0.0) {
-        load_chunk(draft_row(cur), a.vocab, chunk * kChunk, lane, x);
-        const Stat qs = draft_stat[cur];
+      for (int e = 0; e < 4; ++e) w[e] = prob(ps, p[e]);
+      if (less) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = fmax(w[e] - tt * prob(qs, x[e]), 0.0);
+        for (int e = 0; e < 4; ++e) w[e] = fmax(__builtin_fma(-st.t, prob(qs, q[e]), w[e]), 0.0);
       }
-    } else if (cut) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const uint32_t at = 256 * (e / 4) + 4 * lane + e % 4;
-        if (hidden[at / 32] >> (at % 32) & 1) w[e] = 0.0;
-      }
+      put(i, w);
     }
-  };
-  auto chunk_sum = [&](const double (&w)[16]) {
-    double v = 0.0;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v += w[e];
-    return wave_sum64(v);
-  };
-  // the whole of sums, in a fixed order
-  auto whole = [&]() {
-    double v = 0.0;
-    for (uint32_t c = lane; c < chunks; c += 64) v += sums[c];
-    return wave_sum64(v);
-  };
-  // the chunk's tokens among the node's children before `end`, as bits
-  auto hide = [&](uint32_t chunk, uint32_t end) {
-    __syncthreads();
-    if (tid < kChunk / 32) hidden[tid] = 0;
-    __syncthreads();
-    if (tid < end && up[tid] == int32_t(cur) && uint32_t(token[tid]) / kChunk == chunk)
-      atomicOr(&hidden[uint32_t(token[tid]) % kChunk / 32], 1u << (token[tid] & 31));
-    __syncthreads();
-  };
+  }
 
-  while (true) {
-    const Stat here = target_stat[cur];
-    if (here.best < 0) break;
-    uint32_t c = child(cur, last);
-    if (greedy) {
-      while (c < count && token[c] != here.best) c = child(cur, c);
-      if (c >= count) {
-        next = here.best;
-        break;
-      }
-      cur = last = c;
-      if (tid == 0) a.path[r.row + int32_t(kept)] = int32_t(c);
-      ++kept;
-      continue;
+  // the sum of a chunk's weights; hidden: without the tokens in tree.hidden
+  __device__ __forceinline__ double chunk_sum(uint32_t chunk, bool hidden) const {
+    float p[16], q[16] = {};
+    if ((chunk + 1) * kChunk <= a.vocab) {
+      const Raw<TT> rp = load_full(target_row(st.cur), chunk, lane);
+      if constexpr (!POINTS) values(load_full(draft_row(st.cur), chunk, lane), q);
+      values(rp, p);
+    } else {
+      load_rest(target_row(st.cur), a.vocab, chunk, lane, p);
+      if constexpr (!POINTS) load_rest(draft_row(st.cur), a.vocab, chunk, lane, q);
     }
-    if (!POINTS && c < count && draft_stat[cur].best < 0) break;
-    bool down = false;
-    for (; c < count; c = child(cur, c)) {
-      last = c;
-      if (uint32_t(token[c]) >= a.vocab) continue;
-      const double q = qx[c];
-      bool again = false;  // an earlier child of the same token was rejected
-      for (uint32_t j = lane; j < c; j += 64)
-        again = again || (up[j] == int32_t(cur) && token[j] == token[c]);
-      again = __any(again);
-      const double rest = again ? 0.0 : fmax(px[c] - t * q, 0.0);
-      if (random_of(c) * mass * q < rest * left) {
-        down = true;
-        break;
+    double sum = 0.0;
+    weights(p, q, [&](int i, double (&w)[4]) {
+      if (POINTS && hidden) {
+        const uint32_t at = 256 * uint32_t(i) + 4 * lane, bits = tree.hidden[at / 32] >> (at % 32);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = bits >> e & 1 ? 0.0 : w[e];
       }
-      if constexpr (POINTS) {
-        mass = fmax(mass - rest, 0.0);
-      } else {
-        if (left > 0.0) t += mass / left;
-        if (!a.replace && !again) left = fmax(left - q, 0.0);
-        __syncthreads();
-        for (uint32_t k = wave; k < chunks; k += waves) {
-          double w[16];
-          weights(k, t, false, w);
-          const double v = chunk_sum(w);
-          if (lane == 0) sums[k] = v;
+      sum += (w[0] + w[1]) + (w[2] + w[3]);
+    });
+    return wave_sum(sum);
+  }
+
+  // Tests children and goes down until the sums of what is left are needed (true) or
+  // the walk has ended at `next` (false).
+  __device__ __forceinline__ bool walk(int32_t &next) {
+    next = -1;
+#pragma unroll 1
+    while (true) {
+      const Stat here = tree.target[st.cur];
+      if (here.best < 0) return false;
+      uint32_t c = st.child;
+      if (greedy) {
+        while (c != kNone && tree.token[c] != here.best) c = tree.link[c].next;
+        if (c == kNone) {
+          next = here.best;
+          return false;
         }
-        __syncthreads();
-        mass = whole();
+        go_down(c);
+        continue;
       }
-    }
-    if (down) {
-      cur = last = c;
-      if (tid == 0) a.path[r.row + int32_t(kept)] = int32_t(c);
-      ++kept;
-      t = 0.0, mass = 1.0, left = 1.0;
-      continue;
-    }
-    // no child is left: the next token from what remains, or from p where nothing does
-    const bool rejected = last != cur;
-    bool rest = rejected;
-    if (POINTS || t == 0.0 || mass <= 0.0) {
-      if (!POINTS) t = 0.0, rest = false;
-      const Part *const part = a.target_part + (uint64_t(r.row) + cur) * chunks;
-      auto from_parts = [&]() {
-        __syncthreads();
-        for (uint32_t k = tid; k < chunks; k += blockDim.x) {
-          const Part p = part[k];
-          sums[k] = p.max > -INFINITY
-                        ? p.sum * exp_down((double(p.max) - double(here.max)) * inv_temp) * here.inv
-                        : 0.0;
-        }
-        __syncthreads();
-      };
-      from_parts();
-      if (POINTS && rest) {
-        for (uint32_t c2 = child(cur, cur); c2 < count; c2 = child(cur, c2)) {
-          if (uint32_t(token[c2]) >= a.vocab) continue;
-          const uint32_t k = uint32_t(token[c2]) / kChunk;
-          hide(k, count);
-          if (wave == 0) {
-            double w[16];
-            weights(k, 0.0, true, w);
-            const double v = chunk_sum(w);
-            if (lane == 0) sums[k] = v;
+      if (!POINTS && c != kNone && tree.draft[st.cur].best < 0) return false;
+      bool down = false;
+#pragma unroll 1
+      while (c != kNone && st.mass >= kLeast) {
+        const Link link = tree.link[c];
+        const double u = random_of(c), p = tree.px[c], q = tree.qx[c];
+        st.child = link.next;
+        if (!outside(c)) {
+          const double rest = link.again ? 0.0 : fmax(__builtin_fma(-st.t, q, p), 0.0);
+          if (POINTS ? u * st.mass < rest : u * st.mass * q < rest * st.left) {
+            down = true;
+            break;
+          }
+          if constexpr (POINTS) {
+            st.mass = fmax(st.mass - rest, 0.0);
+          } else {
+            if (st.left > 0.0) st.t += st.mass / st.left;
+            if (!a.replace && !link.again) st.left = fmax(st.left - q, 0.0);
+            return true;
           }
         }
-        __syncthreads();
-        if (!(whole() > 0.0)) {
-          rest = false;
-          from_parts();
-        }
+        c = link.next;
       }
+      if (!down) {
+        next = pick(here);
+        return false;
+      }
+      go_down(c);
     }
-    const double limit = random_of(0) * whole();
+  }
+
+  // The token behind the path: from what is left of p, or from p where nothing is.
+  __device__ __forceinline__ int32_t pick(const Stat &here) {
+    const uint32_t chunks = a.chunks;
+    bool hidden = POINTS && st.child != tree.link[st.cur].first;
+    if (!(st.mass >= kLeast)) st.t = 0.0, hidden = false;
+    double *left = sums;  // of each chunk
+    if (!(st.t > 0.0)) {
+      const Part *const part = a.part + (uint64_t(r.row) + st.cur) * chunks;
+      if (chunks <= kLocalChunks) left = &tree.weight[0][0];
+#pragma unroll 1
+      for (uint32_t c = lane; c < chunks; c += 64) {
+        const Part v = part[c];
+        left[c] = v.sum * exp_down(double(v.max) - double(here.max), per_temp) * here.inv;
+      }
+      __threadfence_block();
+      if (hidden) take_out(left);
+    }
+    double total = 0.0;
+#pragma unroll 1
+    for (uint32_t c = lane; c < chunks; c += 64) total += left[c];
+    const double limit = random_of(0) * wave_sum(total);
     // the first chunk whose running sum passes the limit
     double before = 0.0;
     uint32_t at = chunks;
+#pragma unroll 1
     for (uint32_t c0 = 0; c0 < chunks; c0 += 64) {
-      const double v = c0 + lane < chunks ? sums[c0 + lane] : 0.0;
-      double run = v;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(run, d);
-        if (int(lane) >= d) run += o;
-      }
+      const double v = c0 + lane < chunks ? left[c0 + lane] : 0.0;
+      const double run = wave_scan(v);
       const uint64_t m = __ballot(before + run > limit && v > 0.0);
       if (m) {
         const int l = __ffsll((unsigned long long)m) - 1;
         at = c0 + uint32_t(l);
-        before += __shfl(run - v, l);
+        before += lane_value(run - v, l);
         break;
       }
-      before += __shfl(run, 63);
+      before += lane_value(run, 63);
     }
-    if (POINTS && rest && at < chunks) hide(at, count);
-    next = here.best;
-    if (at < chunks) {
-      double w[16];
-      weights(at, t, rest, w);
-      int32_t found = 0x7FFFFFFF, any = -1;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const double v = (w[4 * i] + w[4 * i + 1]) + (w[4 * i + 2] + w[4 * i + 3]);
-        double run = v;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-          const double o = __shfl_up(run, d);
-          if (int(lane) >= d) run += o;
-        }
-        double sum = before + (run - v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int32_t id = int32_t(at * kChunk + 256 * i + 4 * lane + e);
-          sum += w[4 * i + e];
-          if (w[4 * i + e] > 0.0) {
-            any = id;
-            if (sum > limit) found = min(found, id);
-          }
-        }
-        before += __shfl(run, 63);
-      }
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        found = min(found, __shfl_xor(found, d));
-        any = max(any, __shfl_xor(any, d));
-      }
-      // (a rounding may leave the sum at the chunk's end just below the limit)
-      if (found != 0x7FFFFFFF) next = found;
-      else if (any >= 0) next = any;
+    if (at >= chunks) return here.best;
+    if (hidden) hide(at);
+    // its weights, 16 in a row for a lane, and the lane in which the sum passes it
+    float p[16], q[16] = {};
+    const uint32_t first = at * kChunk + 16 * lane;
+    load_run(target_row(st.cur), a.vocab, first, p);
+    if constexpr (!POINTS) {
+      if (st.t > 0.0) load_run(draft_row(st.cur), a.vocab, first, q);
     }
-    break;
+    double sum = 0.0;
+    weights(p, q, [&](int i, double (&w)[4]) {
+      const uint32_t bits = hidden ? tree.hidden[lane / 2] >> (16 * (lane & 1) + 4 * i) : 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = bits >> e & 1 ? 0.0 : w[e];
+        tree.weight[4 * i + e][lane] = w[e];
+        sum += w[e];
+      }
+    });
+    __threadfence_block();
+    const double run = before + wave_scan(sum);
+    // (a rounding may leave the sum at the chunk's end just below the limit: then its
+    // last token with a weight)
+    uint64_t lanes = __ballot(run > limit && sum > 0.0);
+    const bool passes = lanes != 0;
+    if (!passes) lanes = __ballot(sum > 0.0);
+    if (!lanes) return here.best;
+    const int l = passes ? __ffsll((unsigned long long)lanes) - 1 : 63 - __clzll((long long)lanes);
+    const double w = lane < 16 ? tree.weight[lane][l] : 0.0;
+    const double run16 = lane_value(run - sum, l) + wave_scan(w);
+    const uint64_t some = __ballot(w > 0.0), over = __ballot(w > 0.0 && run16 > limit);
+    const int e = passes && over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll((long long)some);
+    return int32_t(at * kChunk) + 16 * l + e;
   }
-  if (tid >= kept && tid < count) a.path[r.row + int32_t(tid)] = -1;
-  if (tid == 0) a.kept[s] = int32_t(kept), a.next[s] = next;
+
+  // A child of `cur` whose token was rejected, the first of that token.
+  __device__ inline bool gone(uint32_t j) const {
+    return j < count && tree.up[j] == int32_t(st.cur) && !outside(j) && !tree.link[j].again;
+  }
+  __device__ inline uint32_t chunk_of(uint32_t j) const { return uint32_t(tree.token[j]) / kChunk; }
+
+  // Takes the rejected points out of the chunks' sums.  Where little of a chunk is left
+  // its tokens are summed up again: the difference would be the sum's rounding.
+  __device__ inline void take_out(double *left) {
+#pragma unroll 1
+    for (uint32_t j0 = 0; j0 < count; j0 += 64) {
+      uint64_t todo = __ballot(gone(j0 + lane));
+#pragma unroll 1
+      while (todo) {
+        const uint32_t chunk = chunk_of(j0 + uint32_t(__ffsll((unsigned long long)todo)) - 1);
+        double out = 0.0;
+        bool earlier = false;  // done with a node of an earlier 64
+#pragma unroll 1
+        for (uint32_t i0 = 0; i0 < count; i0 += 64) {
+          const uint32_t i = i0 + lane;
+          const bool same = gone(i) && chunk_of(i) == chunk;
+          out += same ? tree.px[i] : 0.0;
+          const uint64_t m = __ballot(same);
+          if (i0 < j0 && m) earlier = true;
+          if (i0 == j0) todo &= ~m;
+        }
+        if (earlier) continue;
+        const double all = left[chunk];
+        double rest = all - wave_sum(out);
+        if (!(rest > all * 0x1p-20)) {
+          hide(chunk);
+          rest = chunk_sum(chunk, true);
+        }
+        if (lane == 0) left[chunk] = rest;
+      }
+    }
+    __threadfence_block();
+  }
+
+  // a chunk's tokens among the rejected points, as bits
+  __device__ inline void hide(uint32_t chunk) {
+    if (lane < kChunk / 32) tree.hidden[lane] = 0;
+    __threadfence_block();
+    for (uint32_t j = lane; j < count; j += 64)
+      if (gone(j) && chunk_of(j) == chunk)
+        atomicOr(&tree.hidden[uint32_t(tree.token[j]) % kChunk / 32], 1u << (tree.token[j] & 31));
+    __threadfence_block();
+  }
+
+  __device__ inline void finish(int32_t next) {
+    if (!writes) return;
+    for (uint32_t i = st.kept + lane; i < count; i += 64) a.path[r.row + int32_t(i)] = -1;
+    if (lane == 0) a.kept[s] = int32_t(st.kept), a.next[s] = next;
+  }
+};
+
+// The rows' statistics and the tokens' probabilities, then the walk up to the first
+// rejection of a drawn token, or to its end.
+constexpr uint32_t kWalkThreads = 2 * kMaxNodes;
+
+template <typename TT, typename TD, bool POINTS>
+__global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
+  __shared__ Tree tree;
+  const uint32_t s = blockIdx.x, tid = threadIdx.x;
+  const Rows r = rows_of(a.b, s);
+  if (r.count <= 0) {
+    if (tid == 0) a.kept[s] = 0, a.next[s] = -1, a.state[0][s].waits = 0;
+    return;
+  }
+  Walk<TT, TD, POINTS> w(a, tree, s, r, true, a.sums[0]);
+  const uint32_t count = w.count;
+  // a node's logits: the target's by one half of the block, the draft's by the other
+  const uint32_t node = tid % kMaxNodes;
+  const bool of_draft = tid >= kMaxNodes;
+  const Node me = load_node(a, r, node);
+  const bool drawn = me.up >= 0 && uint32_t(me.token) < a.vocab && !w.greedy && !(POINTS && of_draft);
+  float x = 0.0f;
+  if (drawn) {
+    if (!of_draft) x = logit(w.target_row(uint32_t(me.up)), uint32_t(me.token));
+    else if constexpr (!POINTS) x = logit(w.draft_row(uint32_t(me.up)), uint32_t(me.token));
+  }
+  // (of draft rows without children: statistics of anything, that nothing looks at)
+  const uint32_t rows = (POINTS || w.greedy ? 1 : 2) * count;
+  uint32_t lanes = 64;
+  while (lanes > 8 && rows * lanes > kWalkThreads) lanes /= 2;
+#pragma unroll 1
+  for (uint32_t k = tid / lanes; k < rows; k += kWalkThreads / lanes) {
+    const bool drafted = k >= count;
+    const uint32_t i = drafted ? k - count : k;
+    const Stat st = join_groups((drafted ? a.draft_group : a.target_group) + (uint64_t(r.row) + i) * a.groups,
+                                a.groups, tid % lanes, lanes, w.per_temp);
+    if (tid % lanes == 0) (drafted ? tree.draft : tree.target)[i] = st;
+  }
+  if (!of_draft) tree.put(tid, me);
+  __syncthreads();
+  link_tree(tree, count, tid);
+  if (drawn) (of_draft ? tree.qx : tree.px)[node] = w.prob((of_draft ? tree.draft : tree.target)[me.up], x);
+  __syncthreads();
+  if (!POINTS && tid < count) {
+    const uint64_t row = uint64_t(r.row) + tid;
+    a.px[row] = tree.px[tid], a.qx[row] = tree.qx[tid];
+    a.target_stat[row] = tree.target[tid], a.draft_stat[row] = tree.draft[tid];
+  }
+  if (tid >= 64) return;
+  if (tid == 0) a.path[r.row] = 0;
+  w.st.kept = 1;
+  w.stand_at(0);
+  int32_t next;
+  w.st.waits = w.walk(next);
+  if (!w.st.waits) w.finish(next);
+  if (!POINTS && tid == 0) a.state[0][s] = w.st;
+}
+
+// The rest of a walk.  Pass n: every block of a sequence goes on with the walk by the
+// sums of pass n - 1 (alike, and one of them writes), up to the next rejection, and takes
+// its part of the sums of max(p - t q, 0) that it waits for then.  END: one block a
+// sequence, to the walk's end, by passes of its own where it has to.
+template <typename TT, typename TD, bool END>
+__global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyArgs a, uint32_t n) {
+  __shared__ Tree tree;
+  __shared__ State state;
+  const uint32_t s = blockIdx.y, tid = threadIdx.x, wave = eq_dev::uniform(tid >> 6);
+  const uint32_t before = n ? (n - 1) & 1 : 0;
+  State *const to = a.state[n & 1] + s;
+  const bool writer = blockIdx.x == 0;
+  const State st = a.state[before][s];
+  if (!st.waits) {
+    if (!END && n && writer && tid == 0) to->waits = 0;
+    return;
+  }
+  const Rows r = rows_of(a.b, s);
+  Walk<TT, TD, false> w(a, tree, s, r, writer, a.sums[before]);
+  w.st = st;
+  double *const new_sums = a.sums[n & 1] + uint64_t(s) * a.chunks;
+  auto load_rows = [&](uint32_t i) {
+    const uint64_t row = uint64_t(r.row) + i;
+    tree.target[i] = a.target_stat[row], tree.draft[i] = a.draft_stat[row];
+  };
+  auto pass = [&](uint32_t first, uint32_t step, double *out) {
+#pragma unroll 1
+    for (uint32_t c = first; c < a.chunks; c += step) {
+      const double v = w.chunk_sum(c, false);
+      if (w.lane == 0) out[c] = v;
+    }
+  };
+  if (n == 0) {  // (the walk waits already)
+    if (tid == 0) load_rows(st.cur);
+    __syncthreads();
+  } else {
+    if (tid < kMaxNodes) tree.put(tid, load_node(a, r, tid));
+    if (tid < w.count) {
+      const uint64_t row = uint64_t(r.row) + tid;
+      tree.px[tid] = a.px[row], tree.qx[tid] = a.qx[row];
+      load_rows(tid);
+    }
+    __syncthreads();
+    link_tree(tree, w.count, tid);
+    __syncthreads();
+  }
+#pragma unroll 1
+  while (true) {
+    if (n) {
+      if (wave == 0) {
+        double v = 0.0;
+#pragma unroll 1
+        for (uint32_t c = w.lane; c < a.chunks; c += 64) v += w.sums[c];
+        w.st.mass = wave_sum(v);
+        int32_t next;
+        w.st.waits = w.walk(next);
+        if (!w.st.waits) w.finish(next);
+        if (w.lane == 0) {
+          state = w.st;
+          if (!END && writer) *to = w.st;
+        }
+      }
+      __syncthreads();
+      w.st = state;
+      if (!w.st.waits) return;
+    }
+    if constexpr (!END) {
+      pass(blockIdx.x * 4 + wave, gridDim.x * 4, new_sums);
+      return;
+    }
+    pass(wave, kWalkThreads / 64, w.sums);
+    __syncthreads();
+  }
 }
 
 // ----------------------------------------------------------------------- host
@@ -543,8 +941,6 @@ bool batch_ok(const eq_kv_batch *b) {
 BatchArgs batch_args(const eq_kv_batch *b) {
   return BatchArgs{b->seq_start, b->kv_len, b->n_seqs, b->n_tokens, b->max_new};
 }
-
-uint32_t chunks_of(uint32_t vocab) { return (vocab + kChunk - 1) / kChunk; }
 
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -562,11 +958,74 @@ extern "C" int eq_tree_mask(const eq_kv_batch *batch, const int32_t *parents, ui
   return done();
 }
 
+namespace {
+
+// The parts of a workspace, one behind the other.
+struct Room {
+  uint8_t *at;
+  size_t used = 0;
+  template <typename T>
+  T *take(size_t n) {
+    T *const p = reinterpret_cast<T *>(at + used);
+    used += round256(n * sizeof(T));
+    return p;
+  }
+};
+
+// Splits a batch's rows and a workspace for them; the bytes that it needs.
+size_t lay_out(VerifyArgs &a, bool draft, void *ws) {
+  a.chunks = (a.vocab + kChunk - 1) / kChunk;
+  const uint64_t work = uint64_t(a.chunks) * a.b.n_tokens * (draft ? 2 : 1);
+  a.per = uint32_t(std::min<uint64_t>(std::max<uint64_t>(work / kStatWaves, 1), kMostPer));
+  a.groups = (a.chunks + 4 * a.per - 1) / (4 * a.per);
+  Room room{static_cast<uint8_t *>(ws)};
+  const size_t rows = a.b.n_tokens, seqs = a.b.n_seqs;
+  a.part = room.take<Part>(rows * a.chunks);
+  a.target_group = room.take<Part>(rows * a.groups);
+  a.sums[0] = room.take<double>(seqs * a.chunks);
+  a.state[0] = room.take<State>(seqs);
+  if (draft) {
+    a.sums[1] = room.take<double>(seqs * a.chunks);
+    a.state[1] = room.take<State>(seqs);
+    a.draft_group = room.take<Part>(rows * a.groups);
+    a.px = room.take<double>(rows);
+    a.qx = room.take<double>(rows);
+    a.target_stat = room.take<Stat>(rows);
+    a.draft_stat = room.take<Stat>(rows);
+  }
+  return room.used;
+}
+
+template <typename TT, typename TD>
+void launch_verify(const VerifyArgs &a, uint32_t max_children, hipStream_t stream) {
+  const bool draft = a.draft != nullptr;
+  if (a.b.max_new)
+    hipLaunchKernelGGL((row_stats_kernel<TT, TD>), dim3((draft ? 2 : 1) * a.groups, a.b.max_new, a.b.n_seqs),
+                       dim3(256), 0, stream, a);
+  const dim3 seqs(a.b.n_seqs);
+  if (!draft) {
+    hipLaunchKernelGGL((walk_kernel<TT, TD, true>), seqs, dim3(kWalkThreads), 0, stream, a);
+    return;
+  }
+  hipLaunchKernelGGL((walk_kernel<TT, TD, false>), seqs, dim3(kWalkThreads), 0, stream, a);
+  if (a.b.max_new < 2) return;
+  // a chain's walk ends with its first rejection
+  const uint32_t rounds = max_children == 1 ? 1 : std::min(kRounds, a.b.max_new - 1);
+  const dim3 pass((a.chunks + 3) / 4, a.b.n_seqs);
+  for (uint32_t n = 0; n < rounds; ++n)
+    hipLaunchKernelGGL((pass_kernel<TT, TD, false>), pass, dim3(256), 0, stream, a, n);
+  hipLaunchKernelGGL((pass_kernel<TT, TD, true>), dim3(1, a.b.n_seqs), dim3(kWalkThreads), 0, stream, a,
+                     rounds);
+}
+
+}  // namespace
+
 extern "C" size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, int draft) {
-  if (!batch_ok(batch) || vocab == 0 || vocab > kMaxVocab || batch->n_seqs == 0 || batch->max_new == 0)
-    return 0;
-  const size_t rows = round256(size_t(batch->n_tokens) * chunks_of(vocab) * sizeof(Part));
-  return rows * (draft ? 2 : 1) + round256(size_t(batch->n_seqs) * chunks_of(vocab) * sizeof(double));
+  if (!batch_ok(batch) || vocab == 0 || vocab > kMaxVocab || batch->n_seqs == 0) return 0;
+  VerifyArgs a{};
+  a.b = batch_args(batch);
+  a.vocab = vocab;
+  return lay_out(a, draft != 0, nullptr);
 }
 
 extern "C" int eq_tree_verify(const eq_kv_batch *batch, const int32_t *parents, const int32_t *tokens,
@@ -579,31 +1038,20 @@ extern "C" int eq_tree_verify(const eq_kv_batch *batch, const int32_t *parents, 
       vocab > kMaxVocab || max_children == 0)
     return EQ_EINVAL;
   if (batch->n_seqs == 0) return EQ_OK;
-  if (!kept || !next) return EQ_EINVAL;
-  const size_t need = eq_tree_verify_workspace_bytes(batch, vocab, draft != nullptr);
-  if (batch->max_new && (!parents || !tokens || !target || !random || !path || !ws || ws_bytes < need ||
-                         (reinterpret_cast<uintptr_t>(ws) & 15) ||
-                         (batch->n_tokens > 1 && (target_stride < vocab || (draft && draft_stride < vocab)))))
-    return EQ_EINVAL;
   VerifyArgs a{batch_args(batch), parents, tokens, target, draft, target_stride, draft_stride,
-               temperature, random, path, kept, next, nullptr, nullptr, nullptr, vocab,
-               chunks_of(vocab), replace != 0};
-  const size_t rows = round256(size_t(batch->n_tokens) * a.chunks * sizeof(Part));
-  uint8_t *at = static_cast<uint8_t *>(ws);
-  a.target_part = reinterpret_cast<Part *>(at);
-  if (draft) a.draft_part = reinterpret_cast<Part *>(at += rows);
-  a.sums = reinterpret_cast<double *>(at + rows);
-  const dim3 stats((draft ? 2 : 1) * ((a.chunks + 3) / 4), batch->max_new, batch->n_seqs);
-  const dim3 walk(batch->n_seqs), many(1024);
-  auto go = [&](auto tt, auto td) {
-    using TT = decltype(tt);
-    using TD = decltype(td);
-    if (batch->max_new) hipLaunchKernelGGL((row_stats_kernel<TT, TD>), stats, dim3(256), 0, stream, a);
-    if (draft) hipLaunchKernelGGL((walk_kernel<TT, TD, false>), walk, many, 0, stream, a);
-    else hipLaunchKernelGGL((walk_kernel<TT, TT, true>), walk, many, 0, stream, a);
-  };
+               temperature, random, path, kept, next};
+  a.vocab = vocab;
+  a.replace = replace != 0;
+  const size_t need = lay_out(a, draft != nullptr, ws);
+  if (!kept || !next || !ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15)) return EQ_EINVAL;
+  if (batch->max_new &&
+      (!parents || !tokens || !target || !random || !path ||
+       (batch->n_tokens > 1 && (target_stride < vocab || (draft && draft_stride < vocab)))))
+    return EQ_EINVAL;
   const bool t16 = target_dtype == EQ_BF16, d16 = draft ? draft_dtype == EQ_BF16 : t16;
-  if (t16) d16 ? go(uint16_t{}, uint16_t{}) : go(uint16_t{}, float{});
-  else d16 ? go(float{}, uint16_t{}) : go(float{}, float{});
+  if (t16 && d16) launch_verify<uint16_t, uint16_t>(a, max_children, stream);
+  else if (t16) launch_verify<uint16_t, float>(a, max_children, stream);
+  else if (d16) launch_verify<float, uint16_t>(a, max_children, stream);
+  else launch_verify<float, float>(a, max_children, stream);
   return done();
 }

@@ -75,8 +75,10 @@ def verify(parents, tokens, target, draft, random, temp=1.0, replace=False):
             q = softmax(draft[at], temp)
             if q is None:
                 return path, -1
-        r, went = p, None
+        r, went, left = p, None, 1.0  # left: of p
         for i in kids:
+            if left < 2.0 ** -32:
+                break
             x = int(tokens[i])
             if not 0 <= x < len(p):
                 continue
@@ -96,9 +98,10 @@ def verify(parents, tokens, target, draft, random, temp=1.0, replace=False):
                     q[x] = 0
                     if q.sum() > 0:
                         q = q / q.sum()
+            left *= r.sum()
             if r.sum() > 0:
                 r = r / r.sum()
         if went is None:
-            return path, invert(r if r.sum() > 0 else p, u[0])
+            return path, invert(r if left >= 2.0 ** -32 else p, u[0])
         at = went
         path.append(at)
