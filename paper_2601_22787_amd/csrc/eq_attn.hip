@@ -53,6 +53,7 @@ struct AttnArgs {
   const uint32_t *mask;      // trees: [n_tokens][mask_words], bit j: new token j is seen
   const int32_t *positions;  // trees with a window: [n_tokens]
   uint32_t mask_words;
+  uint32_t *even;            // trees: prompt_kernel's chunk_tiles for join_kernel, or null
 };
 
 // Columns [col0, col0 + COLS) of a sequence, and the cached tokens they see.
@@ -127,6 +128,58 @@ __device__ inline int32_t wave_max(int32_t x) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) x = max(x, __shfl_xor(x, d));
   return x;
+}
+
+// Sums of the lanes up to each.
+__device__ inline uint32_t wave_scan(uint32_t x, uint32_t lane) {
+#pragma unroll
+  for (uint32_t d = 1; d < 64; d *= 2) {
+    const uint32_t o = uint32_t(__shfl_up(int(x), d));
+    x += lane >= d ? o : 0u;
+  }
+  return x;
+}
+__device__ inline uint32_t wave_sum(uint32_t x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x += uint32_t(__shfl_xor(int(x), d));
+  return x;
+}
+
+// What block `number` of a head does for a batch of trees, up to 64 of them: the host
+// knows no lengths, so chunks of one length are set here that make about as many blocks
+// as run at once, and these are numbered without gaps (blocks go round the shader
+// engines by their numbers: with gaps some got twice the work of others).  Two sequences
+// of 32768 tokens and 64 nodes, 64 heads on 8: 159 -> 154 us; three of 25529 to 32768
+// tokens and 19 to 64 nodes 190 -> 168.  A sequence for a lane.
+struct Share {
+  uint32_t seq, qt, chunk, chunk_tiles;
+  bool any;
+};
+
+__device__ inline Share even_share(const AttnArgs &a, uint32_t number) {
+  const View &w = a.w;
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t tiles = 0, q_tiles = 0;
+  if (lane < w.n_seqs) {
+    const Seq q = sequence(w, lane);
+    const uint32_t first = uint32_t(start_of(a.window, max(q.base, 0))) / kPromptTile;
+    tiles = max((uint32_t(q.len) + kPromptTile - 1) / kPromptTile, first) - first;
+    q_tiles = (uint32_t(q.count) * a.group + kPromptCols - 1) / kPromptCols;
+  }
+  const uint32_t run = max(2 * kFillBlocks / w.kv_heads, 1u);  // blocks of a head
+  uint32_t ct = max(a.chunk_tiles, (wave_sum(q_tiles * tiles) + run - 1) / run);
+  auto blocks = [&]() { return max((tiles + ct - 1) / ct, 1u) * q_tiles; };
+  for (int i = 0; i < 12 && wave_sum(blocks()) > run; ++i) ct += (ct + 15) / 16;
+  const uint32_t mine = blocks(), end = wave_scan(mine, lane);
+  const uint64_t m = __ballot(number < end);
+  Share r{0, 0, 0, ct, m != 0};
+  if (!m) return r;
+  r.seq = uint32_t(__ffsll((unsigned long long)m)) - 1;
+  const uint32_t at = number - uint32_t(__builtin_amdgcn_readlane(int(end - mine), int(r.seq)));
+  const uint32_t each = uint32_t(__builtin_amdgcn_readlane(int(mine), int(r.seq)));
+  const uint32_t chunks = each / uint32_t(__builtin_amdgcn_readlane(int(q_tiles), int(r.seq)));
+  r.chunk = at % chunks, r.qt = at / chunks;
+  return r;
 }
 
 // x / scale as two E4M3 terms, of four values: h at `scale`, l at scale / 32 (what h
@@ -676,12 +729,21 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
                      kOdd = kW + kPromptTile * 4, kBuf = kOdd + 16;
   __shared__ __attribute__((aligned(16))) uint8_t lds[3 * kBuf];
   const View &w = a.w;
-  const uint32_t s = blockIdx.y;
+  uint32_t s = blockIdx.y;
   // heads first (blocks go round the 8 XCDs, so with a multiple of 8 heads those of
   // a head share one, whose L2 then holds its cache), and a sequence's last
   // queries, which see most, before its first
   const uint32_t h = blockIdx.x % w.kv_heads, rest = blockIdx.x / w.kv_heads;
-  const uint32_t chunk = rest % a.chunks, qt = a.q_tiles - 1 - rest / a.chunks;
+  uint32_t chunk = rest % a.chunks, qt = a.q_tiles - 1 - rest / a.chunks;
+  if constexpr (TREE) {
+    if (a.even) {
+      const Share e = even_share(a, s * (gridDim.x / w.kv_heads) + rest);
+      if (blockIdx.x == 0 && s == 0 && threadIdx.x == 0) *a.even = e.chunk_tiles;
+      if (!e.any) return;
+      a.chunk_tiles = eq_dev::uniform(e.chunk_tiles);
+      s = eq_dev::uniform(e.seq), qt = eq_dev::uniform(e.qt), chunk = eq_dev::uniform(e.chunk);
+    }
+  }
   const Seq q = sequence(w, s);
   const uint32_t col0 = qt * kPromptCols;
   const Span sp = span_of<kPromptCols, kPromptTile, TREE>(a, q, col0);
@@ -991,6 +1053,7 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   const uint32_t token = blockIdx.x / heads, head = blockIdx.x % heads;
   const Seq q = sequence(w, s);
   if (int32_t(token) >= q.count) return;
+  if (TREE && a.even) a.chunk_tiles = *a.even;
   const uint32_t h = head / a.group, index = token * a.group + head % a.group;
   const uint32_t qt = index / COLS;
   const Span sp = span_of<COLS, TILE, TREE>(a, q, qt * COLS);
@@ -1048,8 +1111,10 @@ size_t part_cols(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
   return size_t(b->n_seqs) * c->kv_heads * p.q_tiles * p.chunks * p.cols;
 }
 
+template <bool TREE>
 size_t attn_bytes(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
-  return p.chunks <= 1 ? 0 : part_cols(p, c, b) * (c->head_dim + 2) * sizeof(float);
+  const size_t even = TREE ? sizeof(uint32_t) : 0;
+  return p.chunks <= 1 ? 0 : part_cols(p, c, b) * (c->head_dim + 2) * sizeof(float) + even;
 }
 
 template <int D, bool TREE>
@@ -1088,13 +1153,14 @@ bool size_ok(const eq_kv_cache *c, const eq_kv_batch *b, uint32_t q_heads) {
   return uint64_t(c->kv_heads) * p.q_tiles * p.chunks <= kMaxBlocks;
 }
 
+template <bool TREE>
 size_t workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch, uint32_t q_heads) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || batch->n_seqs == 0 ||
       batch->max_new == 0 || !size_ok(cache, batch, q_heads))
     return 0;
-  return attn_bytes(plan_attn(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads,
-                              batch->max_new, batch->max_len, 0),
-                    cache, batch);
+  return attn_bytes<TREE>(plan_attn(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads,
+                                    batch->max_new, batch->max_len, 0),
+                          cache, batch);
 }
 
 template <bool TREE>
@@ -1114,13 +1180,15 @@ int attention(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t
   if (!size_ok(cache, batch, q_heads)) return EQ_EINVAL;
   const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len,
                            window);
-  const size_t need = attn_bytes(p, cache, batch);
+  const size_t need = attn_bytes<TREE>(p, cache, batch);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return EQ_EINVAL;
   AttnArgs a{view(cache, batch), q, q_stride, out, static_cast<float *>(ws), nullptr, group, window,
              p.q_tiles, p.chunks, p.chunk_tiles, scale * 1.44269504088896340736f, mask, positions,
-             (batch->max_new + 31) / 32};
+             (batch->max_new + 31) / 32, nullptr};
   if (need)
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
+  if (TREE && need && p.prompt && batch->n_seqs <= 64)
+    a.even = reinterpret_cast<uint32_t *>(a.stat + part_cols(p, cache, batch));
   const dim3 grid(cache->kv_heads * p.q_tiles * p.chunks, batch->n_seqs);
   const dim3 join(batch->max_new * q_heads, batch->n_seqs);
   // a tile in one page has one page number to read and take addresses from (284 000
@@ -1140,7 +1208,7 @@ int attention(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t
 
 extern "C" size_t eq_attn_kv4_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
                                               uint32_t q_heads) {
-  return workspace_bytes(cache, batch, q_heads);
+  return workspace_bytes<false>(cache, batch, q_heads);
 }
 
 extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
@@ -1152,7 +1220,7 @@ extern "C" int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, c
 
 extern "C" size_t eq_attn_kv4_tree_workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch,
                                                    uint32_t q_heads) {
-  return batch && batch->max_new > kMaxNodes ? 0 : workspace_bytes(cache, batch, q_heads);
+  return batch && batch->max_new > kMaxNodes ? 0 : workspace_bytes<true>(cache, batch, q_heads);
 }
 
 extern "C" int eq_attn_kv4_tree(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
