@@ -123,9 +123,16 @@ struct State {
   uint32_t waits;        // for the sums of max(p - t q, 0)
 };
 
+// A node's place among the others.
+struct Link {
+  uint16_t first, next;  // its first child, the next child of its parent; kNone
+  uint32_t again;        // an earlier child of its parent has the same token
+};
+constexpr uint32_t kNone = 0xFFFF;
+
 constexpr double kLeast = 0x1p-32;  // of p: less is taken for nothing
 constexpr uint32_t kRounds = 4;
-constexpr uint32_t kStatWaves = 6144, kMostPer = 3;
+constexpr uint32_t kStatWaves = 3072, kMostPer = 3;
 
 struct VerifyArgs {
   BatchArgs b;
@@ -140,6 +147,7 @@ struct VerifyArgs {
   double *sums[2];                 // [n_seqs][chunks], of even and odd passes
   double *px, *qx;                 // [n_tokens]
   Stat *target_stat, *draft_stat;  // [n_tokens]
+  Link *link;                      // [n_tokens]
   State *state[2];                 // [n_seqs], behind even and odd passes
   uint32_t vocab, chunks, per, groups;
   bool replace;
@@ -208,50 +216,46 @@ __device__ inline float logit(const T *row, uint32_t i) {
   else return eq_dev::bf16_to_f32(row[i]);
 }
 
-// A lane's 16 logits of a chunk: element 4 i + e is number 256 i + 4 lane + e.  Rows
-// start at any element.  In two parts, so that loads stay in flight: what was loaded,
-// and its values.  (A load under a condition would be waited for where the branches
-// meet.)
+// A lane's 16 logits of a chunk, four in a row: number `first + step i + e` is element 4 i
+// + e, with first = 4 lane and step = 256, or 16 lane and 4.  Rows start at any element.
+// In two parts, so that loads stay in flight: what was loaded, and its values.  (A load
+// under a condition would be waited for where the branches meet: fours that reach
+// behind the vocabulary are read before its end and moved up.)
 template <typename T>
 struct Raw {
   T v[4][4];
 };
 template <typename T>
-__device__ inline Raw<T> load_full(const T *row, uint32_t chunk, uint32_t lane) {
+__device__ inline Raw<T> load16(const T *row, uint32_t vocab, uint32_t first, uint32_t step) {
   Raw<T> r;
+  if (vocab >= 4) {
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
-    __builtin_memcpy(r.v[i], row + chunk * kChunk + 256 * i + 4 * lane, sizeof(r.v[i]));
+    for (uint32_t i = 0; i < 4; ++i)
+      __builtin_memcpy(r.v[i], row + min(first + step * i, vocab - 4), sizeof(r.v[i]));
+  } else {
+    T v[3];
+#pragma unroll
+    for (uint32_t e = 0; e < 3; ++e) v[e] = row[min(e, vocab - 1)];
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i) r.v[i / 4][i % 4] = v[min(i % 4, 2u)];
+  }
   return r;
 }
+// cut: some are behind the vocabulary, and become -infinity.
 template <typename T>
-__device__ inline void values(const Raw<T> &r, float (&x)[16]) {
+__device__ inline void values(const Raw<T> &r, uint32_t vocab, uint32_t first, uint32_t step, bool cut,
+                              float (&x)[16]) {
 #pragma unroll
   for (uint32_t i = 0; i < 16; ++i) x[i] = logit(r.v[i / 4], i % 4);
-}
-// The last chunk, -infinity behind the vocabulary.
-template <typename T>
-__device__ inline void load_rest(const T *row, uint32_t vocab, uint32_t chunk, uint32_t lane,
-                                 float (&x)[16]) {
+  if (!cut) return;
 #pragma unroll
-  for (uint32_t i = 0; i < 16; ++i) {
-    const uint32_t at = chunk * kChunk + 256 * (i / 4) + 4 * lane + i % 4;
-    const float v = logit(row, min(at, vocab - 1));
-    x[i] = at < vocab ? v : -INFINITY;
-  }
-}
-
-// 16 logits in a row, -infinity behind the vocabulary.
-template <typename T>
-__device__ inline void load_run(const T *row, uint32_t vocab, uint32_t at, float (&x)[16]) {
-  if (at + 16 <= vocab) {
-    T v[16];
-    __builtin_memcpy(v, row + at, sizeof(v));
+  for (uint32_t i = 0; i < 4; ++i) {
+    const uint32_t at = first + step * i, up = vocab >= 4 ? at - min(at, vocab - 4) : 0;
+    float *const y = x + 4 * i;
+    if (up & 1) y[0] = y[1], y[1] = y[2], y[2] = y[3];
+    if (up & 2) y[0] = y[2], y[1] = y[3];
 #pragma unroll
-    for (uint32_t e = 0; e < 16; ++e) x[e] = logit(v, e);
-  } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 16; ++e) x[e] = at + e < vocab ? logit(row, at + e) : -INFINITY;
+    for (uint32_t e = 0; e < 4; ++e) y[e] = at + e < vocab ? y[e] : -INFINITY;
   }
 }
 
@@ -335,20 +339,16 @@ __device__ inline Part largest(const float (&x)[16], uint32_t chunk, float top) 
 template <typename T>
 __device__ __forceinline__ void row_stats(const T *row, uint32_t vocab, uint32_t chunk, uint32_t end,
                                           uint32_t lane, float temp, double per_temp, Part *out) {
-  const uint32_t full = min(end, vocab / kChunk);  // behind those, one at most
   const bool greedy = !(temp > 0.0f);
-  Raw<T> raw;
-  if (chunk < full) raw = load_full(row, chunk, lane);
+  auto load = [&](uint32_t c) { return load16(row, vocab, c * kChunk + 4 * lane, 256); };
   Power power(INFINITY, per_temp, double(temp));  // (near nothing)
+  Raw<T> raw;
+  if (chunk < end) raw = load(chunk);
 #pragma unroll 1
   for (; chunk < end; ++chunk, ++out) {
     float x[16];
-    if (chunk < full) {
-      values(raw, x);
-      raw = load_full(row, min(chunk + 1, full - 1), lane);
-    } else {
-      load_rest(row, vocab, chunk, lane, x);
-    }
+    values(raw, vocab, chunk * kChunk + 4 * lane, 256, (chunk + 1) * kChunk > vocab, x);
+    raw = load(min(chunk + 1, end - 1));
     float high = x[0], low = x[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) high = fmaxf(high, x[e]), low = fminf(low, x[e]);
@@ -399,7 +399,7 @@ __device__ inline Part join_lanes(Part p, bool on, double per_temp) {
 }
 
 template <typename TT, typename TD>
-__global__ __launch_bounds__(256) void row_stats_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(256, 5) void row_stats_kernel(VerifyArgs a) {
   __shared__ Part parts[4 * kMostPer];
   const uint32_t s = blockIdx.z, i = blockIdx.y;
   const bool drafted = blockIdx.x >= a.groups;
@@ -477,13 +477,6 @@ __device__ inline Stat join_groups(const Part *part, uint32_t groups, uint32_t l
   return Stat{1.0 / sum, all, bad || all == -INFINITY ? -1 : arg};
 }
 
-// A node's place among the others.
-struct Link {
-  uint16_t first, next;  // its first child, the next child of its parent; kNone
-  uint32_t again;        // an earlier child of its parent has the same token
-};
-constexpr uint32_t kNone = 0xFFFF;
-
 struct Node {
   int32_t up, token;  // up: -2 for what hangs on nothing
   float random;
@@ -513,27 +506,44 @@ __device__ inline Node load_node(const VerifyArgs &a, const Rows &r, uint32_t i)
   return Node{on && i > 0 && p >= 0 && p < int32_t(i) ? p : -2, a.tokens[row], a.random[row]};
 }
 
-// The nodes' links, a thread each: a node looks through the later ones, four at a time.
-__device__ inline void link_tree(Tree &tree, uint32_t count, uint32_t tid) {
-  if (tid >= count) return;
-  const int32_t up = tree.up[tid], token = tree.token[tid];
-  uint32_t first = kNone, next = kNone;
-#pragma unroll 1
-  for (uint32_t j0 = (tid + 1) / 4 * 4; j0 < count; j0 += 4) {
-    const int4 u = *reinterpret_cast<const int4 *>(tree.up + j0);
-    const int4 k = *reinterpret_cast<const int4 *>(tree.token + j0);
-    const int32_t us[4] = {u.x, u.y, u.z, u.w}, ks[4] = {k.x, k.y, k.z, k.w};
+// The nodes' links: a wavefront takes every `waves`-th node and finds its children, whose
+// parents its lanes hold, by a ballot.
+__device__ inline void link_tree(Tree &tree, uint32_t count, uint32_t wave, uint32_t waves, uint32_t lane) {
+  constexpr uint32_t kSets = kMaxNodes / 64;
+  const uint32_t sets = (count + 63) / 64;
+  int32_t up[kSets], token[kSets];
 #pragma unroll
-    for (uint32_t e = 0; e < 4; ++e) {
-      const uint32_t j = j0 + e;
-      if (us[e] == int32_t(tid)) first = min(first, j);
-      if (j > tid && us[e] == up && up >= 0) {
-        next = min(next, j);
-        if (ks[e] == token) tree.link[j].again = 1;
+  for (uint32_t b = 0; b < kSets; ++b) {
+    up[b] = b < sets ? tree.up[64 * b + lane] : -2;
+    token[b] = b < sets ? tree.token[64 * b + lane] : 0;
+  }
+#pragma unroll 1
+  for (uint32_t i = wave; i < count; i += waves) {
+    uint64_t kids[kSets];
+    uint32_t behind = kNone;  // the first child of the sets behind
+#pragma unroll
+    for (uint32_t b = kSets; b-- > 0;) {
+      const bool mine = up[b] == int32_t(i);
+      kids[b] = b < sets ? __ballot(mine) : 0;
+      if (!kids[b]) continue;
+      const uint64_t later = kids[b] & ~((uint64_t(2) << lane) - 1);
+      if (mine)
+        tree.link[64 * b + lane].next =
+            uint16_t(later ? 64 * b + uint32_t(__ffsll((unsigned long long)later)) - 1 : behind);
+      behind = 64 * b + uint32_t(__ffsll((unsigned long long)kids[b])) - 1;
+    }
+    if (lane == 0) tree.link[i].first = uint16_t(behind);
+#pragma unroll
+    for (uint32_t b = 0; b < kSets; ++b) {
+      for (uint64_t left = kids[b]; left; left &= left - 1) {
+        const uint32_t c = uint32_t(__ffsll((unsigned long long)left)) - 1;
+        const int32_t t = __builtin_amdgcn_readlane(token[b], int(c));
+#pragma unroll
+        for (uint32_t d = b; d < kSets; ++d)
+          if (up[d] == int32_t(i) && token[d] == t && (d > b || lane > c)) tree.link[64 * d + lane].again = 1;
       }
     }
   }
-  tree.link[tid].first = uint16_t(first), tree.link[tid].next = uint16_t(next);
 }
 
 // A wavefront's walk through a tree.
@@ -581,6 +591,16 @@ struct Walk {
     stand_at(c);
   }
 
+  // 16 logits of the node's target and, where it counts, its draft
+  __device__ __forceinline__ void load(uint32_t first, uint32_t step, bool cut, float (&p)[16],
+                                       float (&q)[16]) const {
+    const Raw<TT> rp = load16(target_row(st.cur), a.vocab, first, step);
+    if constexpr (!POINTS) {
+      if (st.t > 0.0) values(load16(draft_row(st.cur), a.vocab, first, step), a.vocab, first, step, cut, q);
+    }
+    values(rp, a.vocab, first, step, cut, p);
+  }
+
   // The weights max(p - t q, 0) of 16 tokens, four at a time: put(i, w).
   template <typename F>
   __device__ inline void weights(float (&p)[16], float (&q)[16], F &&put) const {
@@ -602,14 +622,7 @@ struct Walk {
   // the sum of a chunk's weights; hidden: without the tokens in tree.hidden
   __device__ __forceinline__ double chunk_sum(uint32_t chunk, bool hidden) const {
     float p[16], q[16] = {};
-    if ((chunk + 1) * kChunk <= a.vocab) {
-      const Raw<TT> rp = load_full(target_row(st.cur), chunk, lane);
-      if constexpr (!POINTS) values(load_full(draft_row(st.cur), chunk, lane), q);
-      values(rp, p);
-    } else {
-      load_rest(target_row(st.cur), a.vocab, chunk, lane, p);
-      if constexpr (!POINTS) load_rest(draft_row(st.cur), a.vocab, chunk, lane, q);
-    }
+    load(chunk * kChunk + 4 * lane, 256, (chunk + 1) * kChunk > a.vocab, p, q);
     double sum = 0.0;
     weights(p, q, [&](int i, double (&w)[4]) {
       if (POINTS && hidden) {
@@ -713,10 +726,7 @@ struct Walk {
     // its weights, 16 in a row for a lane, and the lane in which the sum passes it
     float p[16], q[16] = {};
     const uint32_t first = at * kChunk + 16 * lane;
-    load_run(target_row(st.cur), a.vocab, first, p);
-    if constexpr (!POINTS) {
-      if (st.t > 0.0) load_run(draft_row(st.cur), a.vocab, first, q);
-    }
+    load(first, 4, (at + 1) * kChunk > a.vocab, p, q);
     double sum = 0.0;
     weights(p, q, [&](int i, double (&w)[4]) {
       const uint32_t bits = hidden ? tree.hidden[lane / 2] >> (16 * (lane & 1) + 4 * i) : 0;
@@ -838,13 +848,14 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
   }
   if (!of_draft) tree.put(tid, me);
   __syncthreads();
-  link_tree(tree, count, tid);
+  link_tree(tree, count, eq_dev::uniform(tid >> 6), kWalkThreads / 64, tid & 63);
   if (drawn) (of_draft ? tree.qx : tree.px)[node] = w.prob((of_draft ? tree.draft : tree.target)[me.up], x);
   __syncthreads();
   if (!POINTS && tid < count) {
     const uint64_t row = uint64_t(r.row) + tid;
     a.px[row] = tree.px[tid], a.qx[row] = tree.qx[tid];
     a.target_stat[row] = tree.target[tid], a.draft_stat[row] = tree.draft[tid];
+    a.link[row] = tree.link[tid];
   }
   if (tid >= 64) return;
   if (tid == 0) a.path[r.row] = 0;
@@ -897,9 +908,8 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
       const uint64_t row = uint64_t(r.row) + tid;
       tree.px[tid] = a.px[row], tree.qx[tid] = a.qx[row];
       load_rows(tid);
+      tree.link[tid] = a.link[row];
     }
-    __syncthreads();
-    link_tree(tree, w.count, tid);
     __syncthreads();
   }
 #pragma unroll 1
@@ -992,6 +1002,7 @@ size_t lay_out(VerifyArgs &a, bool draft, void *ws) {
     a.qx = room.take<double>(rows);
     a.target_stat = room.take<Stat>(rows);
     a.draft_stat = room.take<Stat>(rows);
+    a.link = room.take<Link>(rows);
   }
   return room.used;
 }
