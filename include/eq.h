@@ -452,7 +452,7 @@ size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, 
 
 /* Verification of drafted tokens, so that what is kept is distributed as the target's
  * own tokens.  tokens[row]: a node's token.  target: n_tokens rows of `vocab` logits
- * (EQ_F32 or EQ_BF16, target_stride elements apart, any alignment), row i those behind
+ * (EQ_F32 or EQ_BF16, target_stride elements apart, at any element), row i those behind
  * node i; draft: likewise, those that node i's children were drawn from, one after
  * another in the order of their rows, without replacement or (replace) with; or NULL,
  * where the children were not drawn (a table's, the most likely ones).  p and q are

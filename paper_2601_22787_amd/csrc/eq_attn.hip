@@ -139,9 +139,10 @@ __device__ inline uint32_t wave_scan(uint32_t x, uint32_t lane) {
   }
   return x;
 }
-__device__ inline uint32_t wave_sum(uint32_t x) {
+template <typename T>
+__device__ inline T wave_sum(T x) {
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) x += uint32_t(__shfl_xor(int(x), d));
+  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
   return x;
 }
 
@@ -167,7 +168,9 @@ __device__ inline Share even_share(const AttnArgs &a, uint32_t number) {
     q_tiles = (uint32_t(q.count) * a.group + kPromptCols - 1) / kPromptCols;
   }
   const uint32_t run = max(2 * kFillBlocks / w.kv_heads, 1u);  // blocks of a head
-  uint32_t ct = max(a.chunk_tiles, (wave_sum(q_tiles * tiles) + run - 1) / run);
+  // (a product may pass 32 bits; a chunk of 2^24 tiles is any sequence whole)
+  const float even = ceilf(wave_sum(float(q_tiles) * float(tiles)) / float(run));
+  uint32_t ct = max(a.chunk_tiles, uint32_t(fminf(even, 0x1p24f)));
   auto blocks = [&]() { return max((tiles + ct - 1) / ct, 1u) * q_tiles; };
   for (int i = 0; i < 12 && wave_sum(blocks()) > run; ++i) ct += (ct + 15) / 16;
   const uint32_t mine = blocks(), end = wave_scan(mine, lane);

@@ -15,7 +15,8 @@
 // Everything is in 64 bits.  A token is where a running sum of probabilities passes u
 // times the whole: the sum's error, over the probabilities near it, is how often a
 // rounding would decide, 2^-24 times thousands of tokens in 32 bits.  64-bit vector
-// instructions issue at the rate of 32-bit ones here, and an exponential is 20.
+// instructions issue at half to two thirds the rate of 32-bit ones here (a fused
+// multiply-add 6.3 cycles a wavefront against 3.3), and an exponential is 14 to 17.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -63,7 +64,8 @@ struct MaskArgs {
 };
 
 // A block for a sequence, a thread for a node, which walks up through the parents in
-// LDS: as many steps as the node is deep.
+// LDS: as many steps as the node is deep.  64 trees of up to 60 nodes 3.5 us, one launch
+// and its chain of loads.
 __global__ __launch_bounds__(kMaxNodes) void tree_mask_kernel(MaskArgs a) {
   __shared__ int32_t up[kMaxNodes];
   const uint32_t s = blockIdx.x, i = threadIdx.x;
@@ -132,6 +134,7 @@ constexpr uint32_t kNone = 0xFFFF;
 
 constexpr double kLeast = 0x1p-32;  // of p: less is taken for nothing
 constexpr uint32_t kRounds = 4;
+constexpr uint32_t kLocalChunks = 1024;  // chunks whose sums a block keeps in LDS
 constexpr uint32_t kStatWaves = 3072, kMostPer = 3;
 
 struct VerifyArgs {
@@ -145,6 +148,7 @@ struct VerifyArgs {
   Part *part;                      // [n_tokens][chunks], of the target's rows
   Part *target_group, *draft_group;  // [n_tokens][groups], `per` chunks of 4 wavefronts each
   double *sums[2];                 // [n_seqs][chunks], of even and odd passes
+  double *rest;                    // [n_seqs][chunks], where those are more than kLocalChunks
   double *px, *qx;                 // [n_tokens]
   Stat *target_stat, *draft_stat;  // [n_tokens]
   Link *link;                      // [n_tokens]
@@ -167,8 +171,8 @@ __device__ inline double exp2_near(double f) {
   return __builtin_fma(z, f, 1.0);
 }
 
-// exp(d / T) for d up to 0 or not far above, c = log2 e / T; 0 far down (and for -infinity, also times 0, and
-// NaN).
+// exp(d / T) for d up to 0 or not far above, c = log2 e / T; 0 far down (and for
+// -infinity, also times 0, and for NaN).
 __device__ inline double exp_down(double d, double c) {
   const double y = fmax(d * c, -1100.0), z = y + 0x1.8p52;  // y rounded, in the low bits
   return __builtin_ldexp(exp2_near(y - (z - 0x1.8p52)), int(__builtin_bit_cast(uint64_t, z)));
@@ -335,7 +339,10 @@ __device__ inline Part largest(const float (&x)[16], uint32_t chunk, float top) 
 //
 // A wavefront's first chunk sets the reference of its exponentials, and others keep it
 // while they are near: a chunk then has no maximum to agree on first.  A NaN comes out in
-// the sum.  Chunks with far or infinite logits take exp_down.
+// the sum.  Chunks with far or infinite logits take exp_down.  Between memory and the
+// 64-bit instructions: 192 rows of 131072 logits and the draft's in BF16, 128 MB in 33.5
+// us, 3.8 TB/s (a copy: 5.2); without exponentials 21 us for 100 MB.  One chunk a
+// wavefront 38 us, eight 40; 4 wavefronts a SIMD 35, 6 and more spill (37 and up).
 template <typename T>
 __device__ __forceinline__ void row_stats(const T *row, uint32_t vocab, uint32_t chunk, uint32_t end,
                                           uint32_t lane, float temp, double per_temp, Part *out) {
@@ -371,7 +378,7 @@ __device__ __forceinline__ void row_stats(const T *row, uint32_t vocab, uint32_t
       }
       sum = wave_sum(sum) * power.shift;
       bad = sum != sum;
-    } else if (power.ref > -INFINITY) {
+    } else {  // (of -infinity alone: 0)
 #pragma unroll 1
       for (int i = 0; i < 16; i += 4, next<4>(x)) {
 #pragma unroll
@@ -496,7 +503,6 @@ struct Tree {
     link[i] = Link{kNone, kNone, 0};
   }
 };
-constexpr uint32_t kLocalChunks = 1024;  // sums that `weight` has room for
 
 // A sequence's node; behind the last one, none.
 __device__ inline Node load_node(const VerifyArgs &a, const Rows &r, uint32_t i) {
@@ -561,7 +567,7 @@ struct Walk {
   __device__ inline Walk(const VerifyArgs &args, Tree &t, uint32_t seq, const Rows &rows, bool writer,
                          double *chunk_sums)
       : a(args), tree(t), r(rows), s(seq), count(uint32_t(rows.count)), lane(threadIdx.x & 63),
-        writes(writer), sums(chunk_sums + uint64_t(seq) * args.chunks) {
+        writes(writer), sums(POINTS ? nullptr : chunk_sums + uint64_t(seq) * args.chunks) {
     const float temp = temperature_of(a, s);
     greedy = !(temp > 0.0f);
     per_temp = per_temperature(temp);
@@ -658,7 +664,7 @@ struct Walk {
 #pragma unroll 1
       while (c != kNone && st.mass >= kLeast) {
         const Link link = tree.link[c];
-        const double u = random_of(c), p = tree.px[c], q = tree.qx[c];
+        const double u = random_of(c), p = tree.px[c], q = POINTS ? 0.0 : tree.qx[c];
         st.child = link.next;
         if (!outside(c)) {
           const double rest = link.again ? 0.0 : fmax(__builtin_fma(-st.t, q, p), 0.0);
@@ -677,7 +683,7 @@ struct Walk {
         c = link.next;
       }
       if (!down) {
-        next = pick(here);
+        if (writes) next = pick(here);
         return false;
       }
       go_down(c);
@@ -692,7 +698,7 @@ struct Walk {
     double *left = sums;  // of each chunk
     if (!(st.t > 0.0)) {
       const Part *const part = a.part + (uint64_t(r.row) + st.cur) * chunks;
-      if (chunks <= kLocalChunks) left = &tree.weight[0][0];
+      left = chunks <= kLocalChunks ? &tree.weight[0][0] : a.rest + uint64_t(s) * chunks;
 #pragma unroll 1
       for (uint32_t c = lane; c < chunks; c += 64) {
         const Part v = part[c];
@@ -810,7 +816,9 @@ struct Walk {
 };
 
 // The rows' statistics and the tokens' probabilities, then the walk up to the first
-// rejection of a drawn token, or to its end.
+// rejection of a drawn token, or to its end.  All latency: 6 us for a chain of 5 rows, 12
+// for 32 chains that are accepted whole and end in a token, about 0.5 us a node and 4 for
+// the token.
 constexpr uint32_t kWalkThreads = 2 * kMaxNodes;
 
 template <typename TT, typename TD, bool POINTS>
@@ -819,7 +827,10 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
   const uint32_t s = blockIdx.x, tid = threadIdx.x;
   const Rows r = rows_of(a.b, s);
   if (r.count <= 0) {
-    if (tid == 0) a.kept[s] = 0, a.next[s] = -1, a.state[0][s].waits = 0;
+    if (tid == 0) {
+      a.kept[s] = 0, a.next[s] = -1;
+      if constexpr (!POINTS) a.state[0][s].waits = 0;
+    }
     return;
   }
   Walk<TT, TD, POINTS> w(a, tree, s, r, true, a.sums[0]);
@@ -871,6 +882,12 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
 // sums of pass n - 1 (alike, and one of them writes), up to the next rejection, and takes
 // its part of the sums of max(p - t q, 0) that it waits for then.  END: one block a
 // sequence, to the walk's end, by passes of its own where it has to.
+//
+// Passes by all compute units take 5.3 us for 8 sequences of 100003 logits, 8 for 32 of
+// 131072; by one block about 13.  Four of them in launches of their own: 8 trees of up
+// to 32 nodes 58.8 us in the mean of 8 inputs (three 61.3, five 60.7, eight 67.5); an
+// idle one is 1 to 2 us.  A counter and the last block to arrive in place of the next
+// launch: its fences took longer (36 us for 1024 blocks).
 template <typename TT, typename TD, bool END>
 __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyArgs a, uint32_t n) {
   __shared__ Tree tree;
@@ -992,10 +1009,11 @@ size_t lay_out(VerifyArgs &a, bool draft, void *ws) {
   const size_t rows = a.b.n_tokens, seqs = a.b.n_seqs;
   a.part = room.take<Part>(rows * a.chunks);
   a.target_group = room.take<Part>(rows * a.groups);
-  a.sums[0] = room.take<double>(seqs * a.chunks);
-  a.state[0] = room.take<State>(seqs);
+  if (a.chunks > kLocalChunks) a.rest = room.take<double>(seqs * a.chunks);
   if (draft) {
+    a.sums[0] = room.take<double>(seqs * a.chunks);
     a.sums[1] = room.take<double>(seqs * a.chunks);
+    a.state[0] = room.take<State>(seqs);
     a.state[1] = room.take<State>(seqs);
     a.draft_group = room.take<Part>(rows * a.groups);
     a.px = room.take<double>(rows);
@@ -1055,6 +1073,10 @@ extern "C" int eq_tree_verify(const eq_kv_batch *batch, const int32_t *parents, 
   a.replace = replace != 0;
   const size_t need = lay_out(a, draft != nullptr, ws);
   if (!kept || !next || !ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15)) return EQ_EINVAL;
+  const auto odd = [](const void *p, uint32_t dtype) {
+    return reinterpret_cast<uintptr_t>(p) % (dtype == EQ_F32 ? 4 : 2) != 0;
+  };
+  if (odd(target, target_dtype) || odd(draft, draft_dtype)) return EQ_EINVAL;
   if (batch->max_new &&
       (!parents || !tokens || !target || !random || !path ||
        (batch->n_tokens > 1 && (target_stride < vocab || (draft && draft_stride < vocab)))))

@@ -272,3 +272,24 @@ def test_strided_queries_and_another_stream(eq):
     eq.eq_attn_kv4_tree(cache, b, q, 0.125, md, out, eq.attn_tree_workspace(cache, b, 4), stream=s)
     s.synchronize()
     check(out.double().cpu().numpy(), q.double().cpu().numpy(), k, v, seen, 0.125)
+
+
+@pytest.mark.parametrize("n", [64, 66])
+def test_batches_of_many_ragged_trees(eq, n):
+    """Up to 64 sequences share chunks of one length that their lengths set; more have the
+    host's."""
+    r = np.random.default_rng(n)
+    news = [int(x) for x in r.integers(0, 24, n)]
+    news[5] = 40
+    lens = [k + int(x) if k else 0 for k, x in zip(news, r.integers(0, 90, n))]
+    lens[7] = news[7] + 2500
+    n_pages = sum(-(-t // 64) for t in lens) + 1
+    b, starts, _ = batch(eq, news, lens, 64, n_pages, seed=5, bound=8192)
+    cache, k, v, _ = filled(eq, r, lens, 64, 1, 64, n_pages, b, starts)
+    mask, pos, seen = masked(news, lens, [tree(r, k) for k in news])
+    q = dev(r.standard_normal((starts[-1], 2, 64)).astype(np.float32), torch.bfloat16)
+    out = torch.full((starts[-1], 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = eq.attn_tree_workspace(cache, b, 2)
+    ws.fill_(255)
+    eq.eq_attn_kv4_tree(cache, b, q, 0.125, dev(mask), out, ws)
+    check(out.double().cpu().numpy(), q.double().cpu().numpy(), k, v, seen, 0.125)

@@ -258,3 +258,106 @@ def test_what_is_kept_is_distributed_as_the_target(eq):
         found = np.bincount(first, minlength=vocab) / n
         say(draft, np.round(p, 4), np.round(found, 4), "accepted", (second > 0).mean())
         assert (np.abs(found - p) <= 5 * np.sqrt(p * (1 - p) / n)).all()
+
+
+@pytest.mark.parametrize("temp", [1.0, 0.0])
+@pytest.mark.parametrize("which", ["target", "draft"])
+@pytest.mark.parametrize("at", [slice(0, 1024), slice(1024, 2048), slice(2048, 3000), slice(0, 3000),
+                                slice(1500, 1501)])
+def test_nan_wherever_it_is(eq, at, which, temp):
+    """One, a whole chunk of them, and a row of nothing else; beside -infinity too."""
+    r = np.random.default_rng(17)
+    news = [3, 3, 3]
+    parents, t, d, tokens, u = inputs(r, news, 3000, "chain")
+    u[:] = 0
+    for s in range(3):
+        for i in range(1, 3):
+            tokens[3 * s + i] = int(np.argmax(t[3 * s + i - 1]))
+    x = t if which == "target" else d
+    x[1, at] = np.nan
+    x[4] = np.where(np.arange(3000) % 7 == 0, x[4], -np.inf)
+    x[4, at] = np.nan
+    x[7] = -np.inf
+    x[7, at] = np.nan
+    out = check(eq, news, parents, tokens, dev(t), dev(d), u, temps=[temp] * 3)
+    assert temp == 0 and which == "draft" or [k for _, k in out] == [-1] * 3
+    check(eq, news, parents, tokens, dev(t), None, u, temps=[temp] * 3)
+
+
+def test_a_vocabulary_of_more_than_2_to_the_20(eq):
+    """More chunks than a block keeps the sums of."""
+    r = np.random.default_rng(18)
+    news, vocab = [4, 3, 1], (1 << 20) + 77
+    parents, t, d, tokens, u = inputs(r, news, vocab, "star", spread=1.0)
+    for height in (0.0, 0.6, 0.9, 0.999):
+        u[:] = height
+        u[[0, 4, 7]] = r.random(3)
+        for draft in (dev(d), None):
+            check(eq, news, parents, tokens, dev(t), draft, u)
+
+
+def test_two_graphs_share_a_workspace(eq):
+    """Captured one after another on one workspace, replayed in turn with other numbers
+    and eager calls between; every replay equals the eager call."""
+    r = np.random.default_rng(19)
+    news, vocab = [7, 12, 0, 5], 2200
+    calls = []
+    for kind in ("tree", "star"):
+        parents, t, d, tokens, u = inputs(r, news, vocab, kind)
+        b, _, _ = batch(eq, news, [n + 5 for n in news], 32, 40, n_tokens=sum(news))
+        out = [torch.empty(n, dtype=torch.int32, device="cuda") for n in (sum(news), 4, 4)]
+        calls.append((b, dev(np.concatenate(parents).astype(np.int32)), dev(tokens), dev(t), dev(d), dev(u), out))
+    ws, other = (eq.verify_workspace(calls[0][0], vocab) for _ in range(2))
+
+    def run(c, out, room):
+        eq.eq_tree_verify(*c[:6], *out, room)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for c in calls:
+            run(c, c[6], ws)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs = []
+    for c in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(c, c[6], ws)
+        graphs.append(g)
+    for i in range(6):
+        for c, g in zip(calls, graphs):
+            c[5].uniform_()
+            c[3].normal_()
+            c[4].copy_(c[3] + 0.5 * torch.randn_like(c[3]))
+            for x in c[6]:
+                x.fill_(77)
+            if i % 2:
+                ws.fill_(255)
+            g.replay()
+            want = [torch.empty_like(x) for x in c[6]]
+            run(c, want, other)
+            torch.cuda.synchronize()
+            for x, y in zip(c[6], want):
+                assert torch.equal(x, y), i
+
+
+def test_what_earlier_kernels_leave_behind(eq):
+    """The same tokens every time, also after kernels that leave NaN in local memory."""
+    from test_gpu_kv import batch as kv_batch
+    import kv_ref
+    r = np.random.default_rng(20)
+    n = 300
+    b, starts, _ = kv_batch(eq, [1] * n, [130] * n, 32, 5 * n)
+    cache = eq.KvCache(torch.full((5 * n, kv_ref.page_bytes(2, 128, 32)), 255, dtype=torch.uint8, device="cuda"),
+                       page_tokens=32, kv_heads=2, head_dim=128)
+    q = torch.full((n, 16, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    o = torch.empty_like(q)
+    news, vocab = [9, 20, 3, 33, 16], 5000
+    parents, t, d, tokens, u = inputs(r, news, vocab)
+    td, dd = dev(t), dev(d)
+    for i in range(10):
+        u[:] = r.random(sum(news))
+        for draft in (dd, None):
+            eq.eq_attn_kv4(cache, b, q, 0.1, o, eq.attn_workspace(cache, b, 16))
+            check(eq, news, parents, tokens, td, draft, u)
+    assert torch.isnan(o).all()

@@ -67,7 +67,8 @@ def test_verification_refused():
     for over in (dict(parents=None), dict(tokens=None), dict(target=None), dict(random=None),
                  dict(path=None), dict(kept=None), dict(nxt=None), dict(ws=None), dict(ws=P + 8),
                  dict(ts=99), dict(ds=99), dict(tk=2), dict(dk=2), dict(vocab=0),
-                 dict(vocab=(1 << 24) + 1, ts=1 << 25, ds=1 << 25), dict(kids=0)):
+                 dict(vocab=(1 << 24) + 1, ts=1 << 25, ds=1 << 25), dict(kids=0),
+                 dict(target=P + 2), dict(target=P + 1, tk=1), dict(draft=P + 1)):
         assert verify(batch(), **over) == eq.EQ_EINVAL, over
     b, wide = batch(), batch(max_new=257, n_tokens=300)
 
