@@ -188,9 +188,10 @@ __device__ inline Share even_share(const AttnArgs &a, uint32_t number) {
 // x / scale as two E4M3 terms, of four values: h at `scale`, l at scale / 32 (what h
 // leaves of magnitudes below 256 is at most 8, 256 of its units; E4M3 ends at 448).
 __device__ inline void split4(const float *x, float scale, int &h, int &l) {
-  short2v a, b;  // each conversion fills one half
-  a = __builtin_nondeterministic_value(a);
-  b = __builtin_nondeterministic_value(b);
+  int a0, b0;  // each conversion fills one half of a register, whatever it held
+  asm("" : "=v"(a0));
+  asm("" : "=v"(b0));
+  short2v a = __builtin_bit_cast(short2v, a0), b = __builtin_bit_cast(short2v, b0);
   a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, x[0], x[1], scale, false);
   a = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(a, x[2], x[3], scale, true);
   h = __builtin_bit_cast(int, a);
@@ -210,6 +211,23 @@ __device__ inline int top_byte(uint32_t top) {
 }
 __device__ inline int low_byte(int b) { return b == 255 ? 255 : b - 5; }
 __device__ inline float byte_value(int b) { return __uint_as_float(uint32_t(b) << 23); }
+
+// 2^(byte E of bytes - 127), by a shift that takes the byte itself: the compiler has an
+// "and" besides for three of the four, 24 instructions of attn_kernel's tile.
+template <int E>
+__device__ inline float byte_scale(uint32_t bytes) {
+  uint32_t x;
+  const uint32_t shift = 23;
+#define EQ_BYTE(n) \
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_" n \
+      : "=v"(x) : "v"(shift), "v"(bytes))
+  if constexpr (E == 0) EQ_BYTE("0");
+  if constexpr (E == 1) EQ_BYTE("1");
+  if constexpr (E == 2) EQ_BYTE("2");
+  if constexpr (E == 3) EQ_BYTE("3");
+#undef EQ_BYTE
+  return __uint_as_float(x);
+}
 
 __device__ inline float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -342,6 +360,10 @@ __device__ inline int4v load_codes(const uint8_t *p) {
 // join.
 //
 // TREE: a column's new tokens are its mask's, 16 bits of it for 16 tokens in a row.
+// Here 16 columns see a tile of 128 tokens, and the 460 vector instructions of that are
+// the limit: eight trees of 16 nodes, 64 heads on 8, 4096 tokens in 27 us, vector units
+// 0.5 and matrix units 0.2 busy over the whole launch, 8 wavefronts a compute unit at
+// most.  A form of 32 columns a wavefront, with half the loads, took 29 to 32.
 template <int D, bool ONE, bool STREAM, bool PAIR, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int ND = D / 16;
@@ -418,7 +440,6 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   int4v kreg[8], vreg[ND];
   uint4 va, vb;  // (PAIR: va is of the lane's own 16 tokens)
   int ksa, ksb;
-  uint32_t ma[2] = {}, mb[2] = {};  // TREE: mask words of va's and vb's tokens
   auto load_k = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const pa = part_of(d, gk >> 1), *const pb = part_of(d, 2 + (gk >> 1));
     const uint32_t a0 = slot_of(tile, gk >> 1) + 16 * (gk & 1);
@@ -437,18 +458,25 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     va = *reinterpret_cast<const uint4 *>(part_of(d, unit) + (at + slot_of(tile, unit)));
     if constexpr (!PAIR)
       vb = *reinterpret_cast<const uint4 *>(part_of(d, 2 + unit) + (at + slot_of(tile, 2 + unit)));
-    if constexpr (TREE) {
-      const int32_t i = (int32_t(tile * kTile + 16 * g) + (upper ? 64 : 0) - node.base) >> 5;
-      ma[0] = mask_word(a, node.mask, i), ma[1] = mask_word(a, node.mask, i + 1);
-      if constexpr (!PAIR)
-        mb[0] = mask_word(a, node.mask, i + 2), mb[1] = mask_word(a, node.mask, i + 3);
-    }
   };
   auto load_v = [&](uint32_t tile, const Ids &d) {
     const uint8_t *const p = part_of(d, g) + (w.v_off + slot_of(tile, g) * (D / 2) + col * 16);
 #pragma unroll
     for (int m = 0; m < ND; ++m) vreg[m] = load_codes<STREAM>(p + m * 256);
   };
+
+  // TREE: new tokens lie in three tiles at most, so in one of this wavefront's; the
+  // mask words of a lane's tokens there
+  uint32_t ma[2] = {}, mb[2] = {}, new_tile = 0;
+  if constexpr (TREE) {
+    static_assert((eq_kv::kMaxNodes + kTile - 2) / kTile + 1 <= kWaves);
+    const uint32_t tb = uint32_t(max(q.base, 0)) / kTile;
+    new_tile = tb + ((t - tb) & (kWaves - 1));
+    const int32_t i = (int32_t(new_tile * kTile + 16 * g) + (upper ? 64 : 0) - node.base) >> 5;
+    ma[0] = mask_word(a, node.mask, i), ma[1] = mask_word(a, node.mask, i + 1);
+    if constexpr (!PAIR)
+      mb[0] = mask_word(a, node.mask, i + 2), mb[1] = mask_word(a, node.mask, i + 3);
+  }
 
   float m_run = -INFINITY, m_use = 0.0f, l_run = 0.0f;
   int8v ph{}, pq{};  // w P of a tile, as two terms (PAIR: ph is the lane's term)
@@ -519,7 +547,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
           if constexpr (TREE) {
             const int32_t there = min(max(int32_t(sp.seen) - from, 0), 16);
             const uint32_t own = __builtin_amdgcn_alignbit(m[1], m[0], uint32_t(from - node.base) & 31);
-            b |= node.alive ? own & ((1u << there) - 1) : 0u;
+            b |= node.alive && t == new_tile ? own & ((1u << there) - 1) : 0u;
           }
           return gone >> unit & 1 ? 0u : b;
         };
@@ -560,9 +588,10 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[e] = exp2_(__builtin_fmaf(x[i + e], a.c, -m_use));
         l_run += (p[0] + p[1]) + (p[2] + p[3]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[i + e] = p[e] * __uint_as_float((vs[i / 4] >> (8 * e) & 255u) << 23);
+        x[i] = p[0] * byte_scale<0>(vs[i / 4]);
+        x[i + 1] = p[1] * byte_scale<1>(vs[i / 4]);
+        x[i + 2] = p[2] * byte_scale<2>(vs[i / 4]);
+        x[i + 3] = p[3] * byte_scale<3>(vs[i / 4]);
       }
       if (masked) {  // (a value that is NaN has the scale infinity: 0 times that is not 0)
 #pragma unroll
@@ -1109,6 +1138,84 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
       make_uint2(eq_dev::pack_bf16(o.x * inv, o.y * inv), eq_dev::pack_bf16(o.z * inv, o.w * inv));
 }
 
+// The same for a tree's many columns, to the bit: D / 4 lanes take a column, and its
+// chunks in turn.  join_kernel's blocks wait for their loads most of the time: four
+// trees of up to 64 nodes, 64 heads, 15.4 us; here 8.4, of which reading the 29 MB of
+// partial results at a copy's rate would be 6.  With few columns, the lanes that share a
+// column's chunks are faster.  Sequences x nodes x heads, cached tokens: us of a call,
+// join_kernel / here
+//   1 x 16 x 32, 8192: 22.4 / 22.7   1 x 16 x 32, 32768: 33.0 / 36.5
+//   1 x 32 x 64, 8192: 32.7 / 32.2   1 x 128 x 16, 131072: 145.0 / 144.4
+//   4 x 32 x 64, 16384: 90.6 / 85.2  2 x 128 x 64, 16384: 163.7 / 149.7
+constexpr uint64_t kManyRows = 2048;
+
+template <int D>
+__global__ __launch_bounds__(256) void join_rows_kernel(AttnArgs a) {
+  constexpr uint32_t kLanes = D / 4, kParts = 64 / kLanes;
+  const View &w = a.w;
+  const uint32_t s = blockIdx.y, heads = w.kv_heads * a.group, l = threadIdx.x % kLanes;
+  const uint32_t at = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const uint32_t token = at / heads, head = at % heads;
+  const Seq q = sequence(w, s);
+  if (token >= uint32_t(q.count)) return;
+  if (a.even) a.chunk_tiles = *a.even;
+  const uint32_t h = head / a.group, index = token * a.group + head % a.group;
+  const uint32_t qt = index / kPromptCols;
+  const Span sp = span_of<kPromptCols, kPromptTile, true>(a, q, qt * kPromptCols);
+  if (sp.chunks <= 1) return;
+  const uint64_t first = (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * kPromptCols +
+                         index % kPromptCols;
+  auto stat = [&](uint32_t c) {
+    return c < sp.chunks ? a.stat[first + uint64_t(c) * kPromptCols] : make_float2(-INFINITY, 0.0f);
+  };
+  float m = -INFINITY;
+  for (uint32_t c = l; c < sp.chunks; c += kLanes) m = fmaxf(m, stat(c).x);
+#pragma unroll
+  for (uint32_t d = 1; d < kLanes; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+  if (m == -INFINITY) m = 0.0f;
+  // (sums in join_kernel's order: of every eighth chunk, and of 64 lanes)
+  float4 o[8] = {};
+  float total[kParts] = {};
+  for (uint32_t c0 = 0; c0 < sp.chunks; c0 += 64) {
+#pragma unroll
+    for (uint32_t part = 0; part < kParts; ++part) {
+      const uint32_t c1 = c0 + part * kLanes;
+      if (c1 >= sp.chunks) break;
+      const float2 st = stat(c1 + l);
+      const float f = exp2_(st.x - m);
+      total[part] += f * st.y;
+      const uint32_t n = min(sp.chunks - c1, kLanes);
+      for (uint32_t k = 0; k < n; k += 8) {
+        float4 x[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+          x[j] = *reinterpret_cast<const float4 *>(
+              a.part + (first + uint64_t(c1 + min(k + j, n - 1)) * kPromptCols) * D + 4 * l);
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+          const float fc = __shfl(f, int(k + j), int(kLanes));  // 0 behind the last chunk
+          o[j].x += fc * x[j].x, o[j].y += fc * x[j].y, o[j].z += fc * x[j].z, o[j].w += fc * x[j].w;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (uint32_t part = 0; part < kParts; ++part)
+#pragma unroll
+    for (uint32_t d = 1; d < kLanes; d *= 2) total[part] += __shfl_xor(total[part], d);
+#pragma unroll
+  for (uint32_t d = 1; d < kParts; d *= 2)
+#pragma unroll
+    for (uint32_t part = 0; part < kParts; part += 2 * d) total[part] += total[part + d];
+#pragma unroll
+  for (uint32_t j = 1; j < 8; ++j)
+    o[0].x += o[j].x, o[0].y += o[j].y, o[0].z += o[j].z, o[0].w += o[j].w;
+  const float inv = total[0] == 0.0f ? 0.0f : 1.0f / total[0];
+  *reinterpret_cast<uint2 *>(a.out + (uint64_t(q.row + token) * heads + head) * D + 4 * l) =
+      make_uint2(eq_dev::pack_bf16(o[0].x * inv, o[0].y * inv),
+                 eq_dev::pack_bf16(o[0].z * inv, o[0].w * inv));
+}
+
 // Columns of partial results: a sum for each channel, a maximum and a sum of P.
 size_t part_cols(const Plan &p, const eq_kv_cache *c, const eq_kv_batch *b) {
   return size_t(b->n_seqs) * c->kv_heads * p.q_tiles * p.chunks * p.cols;
@@ -1126,9 +1233,13 @@ void launch_attn(const AttnArgs &a, const Plan &p, bool pair, bool one_page, boo
   const dim3 block(256), join_block(2 * D);
   if (p.prompt) {
     hipLaunchKernelGGL((prompt_kernel<D, TREE>), grid, block, 0, stream, a);
-    if (p.chunks > 1)
+    if (p.chunks > 1 && TREE && uint64_t(join.x) * join.y >= kManyRows) {
+      const dim3 rows((join.x + 1024 / D - 1) / (1024 / D), join.y);
+      hipLaunchKernelGGL(join_rows_kernel<D>, rows, block, 0, stream, a);
+    } else if (p.chunks > 1) {
       hipLaunchKernelGGL((join_kernel<D, kPromptCols, kPromptTile, TREE>), join, join_block, 0, stream,
                          a);
+    }
     return;
   }
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };

@@ -17,7 +17,7 @@ constexpr uint32_t kMaxBlocks = (1u << 24) - 1;
 // Offsets within a head's part of a page, and the batch, by value for kernels.
 struct View {
   uint8_t *pages;
-  uint64_t page_bytes;
+  uint32_t page_bytes;  // (below 2^30: 1024 heads, 4096 tokens of 133 bytes)
   uint32_t head_bytes;
   uint32_t v_off, ks_off, vs_off;  // value codes, key scales, value scales
   uint32_t page_shift;             // log2 page_tokens
@@ -49,7 +49,7 @@ inline View view(const eq_kv_cache *c, const eq_kv_batch *b) {
   const uint32_t n = c->page_tokens, d = c->head_dim;
   w.pages = c->pages;
   w.head_bytes = head_bytes(d, n);
-  w.page_bytes = uint64_t(w.head_bytes) * c->kv_heads;
+  w.page_bytes = w.head_bytes * c->kv_heads;
   w.v_off = n * d / 2;
   w.ks_off = n * d;
   w.vs_off = n * d + n * (d / 32);
