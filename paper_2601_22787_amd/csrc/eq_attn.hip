@@ -362,7 +362,7 @@ __device__ inline int4v load_codes(const uint8_t *p) {
 // TREE: a column's new tokens are its mask's, 16 bits of it for 16 tokens in a row.
 // Here 16 columns see a tile of 128 tokens, and the 460 vector instructions of that are
 // the limit: eight trees of 16 nodes, 64 heads on 8, 4096 tokens in 27 us, vector units
-// 0.5 and matrix units 0.2 busy over the whole launch, 8 wavefronts a compute unit at
+// 0.4 and matrix units 0.2 busy over the whole launch, 8 wavefronts a compute unit at
 // most.  A form of 32 columns a wavefront, with half the loads, took 29 to 32.
 template <int D, bool ONE, bool STREAM, bool PAIR, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
