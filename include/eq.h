@@ -419,7 +419,8 @@ int eq_attn_kv4(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16
  *   eq_kv_keep              the path's keys and values to consecutive places, in all
  *                           layers' caches
  * A chain of drafted tokens is a tree of one path.  All of it is on the device and may
- * be captured; max_new is at most EQ_TREE_NODES. */
+ * be captured; max_new is at most EQ_TREE_NODES.  What a call writes lies apart from
+ * what it reads. */
 #define EQ_TREE_NODES 256
 
 /* Masks and positions of trees.  mask: [n_tokens][W] words, W = ceil(max_new / 32)
@@ -489,8 +490,8 @@ int eq_tree_verify(const eq_kv_batch *batch, const int32_t *parents, const int32
  * places takes the key and value of new token path[seq_start[s] + k], for k < kept[s].
  * Entries below k or beyond the sequence's rows, and tokens of pages that are not
  * there, are left out.  Places behind the kept ones hold what they held.  new_len (or
- * NULL; not kv_len itself, which other blocks read): int32 [n_seqs], kv_len less the
- * nodes that were not kept.  Two sequences may share pages, but not 8 aligned positions
+ * NULL): int32 [n_seqs], kv_len less the nodes that were not kept, in memory of its
+ * own (not kv_len's or kept's, which other blocks read).  Two sequences may share pages, but not 8 aligned positions
  * that either moves tokens to. */
 #define EQ_KEEP_CACHES 128
 int eq_kv_keep(const eq_kv_cache *const *caches, uint32_t n, const eq_kv_batch *batch,

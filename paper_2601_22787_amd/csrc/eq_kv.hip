@@ -684,7 +684,16 @@ extern "C" int eq_kv_keep(const eq_kv_cache *const *caches, uint32_t n, const eq
   }
   if (batch->max_new > kMaxNodes) return EQ_EINVAL;
   if (batch->n_seqs == 0) return EQ_OK;
-  if (!kept || (batch->max_new && !path) || new_len == batch->kv_len) return EQ_EINVAL;
+  if (!kept || (batch->max_new && !path)) return EQ_EINVAL;
+  // (one block of a sequence writes its length while the others read these)
+  auto apart = [&](const int32_t *in, uint64_t n) {
+    const uintptr_t o = reinterpret_cast<uintptr_t>(new_len), i = reinterpret_cast<uintptr_t>(in);
+    return o + 4 * uint64_t(batch->n_seqs) <= i || i + 4 * n <= o;
+  };
+  if (new_len && !(apart(batch->kv_len, batch->n_seqs) && apart(kept, batch->n_seqs) &&
+                   apart(batch->seq_start, uint64_t(batch->n_seqs) + 1) &&
+                   (!path || apart(path, batch->n_tokens))))
+    return EQ_EINVAL;
   KeepArgs a{view(caches[0], batch), path, kept, new_len, {}};
   for (uint32_t i = 0; i < n; ++i) a.pages[i] = caches[i]->pages;
   const dim3 grid((caches[0]->kv_heads + 3) / 4, batch->n_seqs, n);

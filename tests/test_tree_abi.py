@@ -96,6 +96,16 @@ def test_keeping_refused():
     assert keep([a, b], batch(n_seqs=0)) == eq.EQ_OK
 
 
+def test_lengths_after_keeping_are_refused_where_the_call_reads():
+    """new_len on kv_len, kept, path or seq_start, or on a part of them."""
+    a, far = cache(), P + (1 << 20)
+    b = batch(n_seqs=4, n_tokens=40, max_new=4, seq_start=far, kv_len=far + 4096)
+    path, kept = far + 8192, far + 12288
+    for new_len in (far, far + 4 * 4, far + 4096, far + 4096 + 12, far + 4096 - 12, path, path + 4 * 39,
+                    path - 12, kept, kept - 4, kept + 12):
+        assert keep([a], b, path, kept, new_len) == eq.EQ_EINVAL, hex(new_len - far)
+
+
 def _call(which, at):
     """One call with every part on cuda:0 but for what `at` names."""
     torch = pytest.importorskip("torch")
