@@ -103,17 +103,25 @@ struct Node {
   bool alive;            // a node, which sees itself at least
 };
 
-__device__ inline Node node_of(const AttnArgs &a, const Seq &q, uint32_t token, bool real) {
-  Node n{a.mask, 0, 0, q.base, false};
-  if (!real || q.base + int32_t(token) < 0) return n;
-  const uint64_t row = uint64_t(q.row) + token;
-  n.mask += row * a.mask_words;
+// words: the column's mask (what a narrower one has behind it, its last word again).
+constexpr int kMaskWords = kMaxNodes / 32;
+__device__ inline Node node_of(const AttnArgs &a, const Seq &q, uint32_t token, bool real,
+                               uint32_t (&words)[kMaskWords]) {
+  const bool on = real && q.base + int32_t(token) >= 0;
+  const uint64_t row = on ? uint64_t(q.row) + token : 0;
+  Node n{a.mask + row * a.mask_words, 0, 0, q.base, false};
+  int32_t pos = 0;
+  if (a.window) pos = a.positions[row];
   uint32_t any = 0;
-  for (uint32_t i = 0; i < a.mask_words; ++i) any |= n.mask[i];
-  if (!any) return n;
+#pragma unroll
+  for (int i = 0; i < kMaskWords; ++i) {  // (one wait for all)
+    words[i] = n.mask[min(uint32_t(i), a.mask_words - 1)];
+    any |= words[i];
+  }
+  if (!on || !any) return n;
   n.alive = true;
   n.hi = min(max(q.base, 0), q.len);
-  if (a.window) n.lo = min(start_of(a.window, max(a.positions[row], max(q.base, 0))), n.hi);
+  if (a.window) n.lo = min(start_of(a.window, max(pos, max(q.base, 0))), n.hi);
   return n;
 }
 
@@ -313,6 +321,9 @@ __device__ inline floatx4 mul16(int8v codes, int8v terms, floatx4 acc, int as, i
 // All ones where bit i of m is set, else 0.
 __device__ inline uint32_t bit_mask(uint32_t m, int i) { return uint32_t(int32_t(m << (31 - i)) >> 31); }
 
+// Bits 0 to n - 1.
+__device__ inline uint32_t bits_below(int32_t n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1; }
+
 // x of the lane 8 columns on (of 16).
 __device__ inline float other_half(float x) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));
@@ -419,7 +430,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   int32_t hi_min = sp.hi_min, lo_max = sp.lo_max;
   Node node{};
   if constexpr (TREE) {
-    node = node_of(a, q, token, real);
+    uint32_t words[kMaskWords];
+    node = node_of(a, q, token, real, words);
     hi = node.hi, lo = node.lo;
     if (__any(real && !node.alive)) hi_min = 0;
     if (a.window) lo_max = wave_max(lo);
@@ -760,6 +772,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   constexpr uint32_t kV = kPromptTile * kRow, kKS = kV + D * kVRow, kW = kKS + 256,
                      kOdd = kW + kPromptTile * 4, kBuf = kOdd + 16;
   __shared__ __attribute__((aligned(16))) uint8_t lds[3 * kBuf];
+  // TREE: the columns' masks (rows of them start in 32 banks), read where a tile has new tokens
+  constexpr uint32_t kMaskRow = kMaskWords + 1;
+  __shared__ uint32_t lds_mask[TREE ? kPromptCols * kMaskRow : 1];
   const View &w = a.w;
   uint32_t s = blockIdx.y;
   // heads first (blocks go round the 8 XCDs, so with a multiple of 8 heads those of
@@ -803,7 +818,11 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
   }
   Node node{};
   if constexpr (TREE) {
-    node = node_of(a, q, token, real);
+    uint32_t words[kMaskWords];
+    node = node_of(a, q, token, real, words);
+#pragma unroll
+    for (int i = 0; i < kMaskWords; ++i)  // (both halves write the same)
+      lds_mask[(wave * 32 + col) * kMaskRow + i] = uint32_t(i) < a.mask_words && node.alive ? words[i] : 0u;
     hi = node.hi, lo = node.lo;
     all_hi = __any(real && !node.alive) ? 0 : sp.hi_min;
     all_lo = a.window ? wave_max(lo) : 0;
@@ -913,19 +932,29 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(AttnArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint32_t gone = u ? odd.z : odd.x, nan = u ? odd.w : odd.y;
-        uint32_t own = 0;  // TREE: the unit's new tokens that are seen
+        const int32_t from = at + 32 * u;
+        uint32_t visible = bits_below(hi - from) & ~bits_below(lo - from);  // of the unit's tokens
         if constexpr (TREE) {
-          const int32_t from = at + 32 * u - node.base, there = int32_t(sp.seen) - at - 32 * u;
-          own = __builtin_amdgcn_alignbit(mask_word(a, node.mask, (from >> 5) + 1),
-                                          mask_word(a, node.mask, from >> 5), uint32_t(from) & 31);
-          if (there < 32) own &= (1u << max(there, 0)) - 1;
-          if (!node.alive) own = 0;
+          auto word = [&](int32_t i) {
+            const uint32_t x = lds_mask[(wave * 32 + col) * kMaskRow + (uint32_t(i) & (kMaskWords - 1))];
+            return uint32_t(i) < uint32_t(kMaskWords) ? x : 0u;
+          };
+          const int32_t first = from - node.base;
+          const uint32_t own =
+              __builtin_amdgcn_alignbit(word((first >> 5) + 1), word(first >> 5), uint32_t(first) & 31);
+          visible |= own & bits_below(int32_t(sp.seen) - from);
+        }
+        if (gone) visible = 0;
+        visible >>= 8 * half;  // this lane's: 0 to 7 and 16 to 23
+        if (eq_dev::uniform(nan)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (nan >> (16 * (i / 8) + 8 * half + i % 8) & 1) sc[u][i] = NAN;
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int32_t in = 16 * (i / 8) + 8 * int32_t(half) + i % 8, tok = at + 32 * u + in;
-          if (nan >> in & 1) sc[u][i] = NAN;
-          if (((tok < lo || tok >= hi) && !(TREE && (own >> in & 1))) || gone) sc[u][i] = -INFINITY;
+          const uint32_t m = bit_mask(visible, 16 * (i / 8) + i % 8);
+          sc[u][i] = __uint_as_float((__float_as_uint(sc[u][i]) & m) | (0xFF800000u & ~m));
         }
       }
     }
