@@ -819,11 +819,21 @@ struct Walk {
 // rejection of a drawn token, or to its end.  All latency: 6 us for a chain of 5 rows, 12
 // for 32 chains that are accepted whole and end in a token, about 0.5 us a node and 4 for
 // the token.
-constexpr uint32_t kWalkThreads = 2 * kMaxNodes;
+//
+// Of few chunks it goes to the walk's end, with passes of its own in place of
+// pass_kernel's launches (5 us each, an idle one 1 to 2).  us of a call with launches /
+// so, sequences x nodes (most children), chunks:
+//   8 x 16 (4), 8: 40.9 / 25.4   32 x 24 (4), 8: 57.6 / 38.7   32 x 6 (1), 8: 30.5 / 21.4
+//   8 x 16 (4), 16: 35.5 / 28.1  32 x 24 (4), 16: 70.4 / 61.5  32 x 6 (1), 16: 33.1 / 27.1
+//   8 x 16 (4), 32: 46.4 / 51.0  32 x 24 (4), 32: 82.5 / 94.9  32 x 6 (1), 32: 38.6 / 38.5
+constexpr uint32_t kWalkThreads = 2 * kMaxNodes, kFewChunks = 16;
+static_assert(kFewChunks <= 64);
 
 template <typename TT, typename TD, bool POINTS>
 __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
   __shared__ Tree tree;
+  __shared__ State state;
+  __shared__ double sums[kFewChunks];
   const uint32_t s = blockIdx.x, tid = threadIdx.x;
   const Rows r = rows_of(a.b, s);
   if (r.count <= 0) {
@@ -862,20 +872,45 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
   link_tree(tree, count, eq_dev::uniform(tid >> 6), kWalkThreads / 64, tid & 63);
   if (drawn) (of_draft ? tree.qx : tree.px)[node] = w.prob((of_draft ? tree.draft : tree.target)[me.up], x);
   __syncthreads();
-  if (!POINTS && tid < count) {
+  const bool few = a.chunks <= kFewChunks;
+  if (!POINTS && !few && tid < count) {
     const uint64_t row = uint64_t(r.row) + tid;
     a.px[row] = tree.px[tid], a.qx[row] = tree.qx[tid];
     a.target_stat[row] = tree.target[tid], a.draft_stat[row] = tree.draft[tid];
     a.link[row] = tree.link[tid];
   }
-  if (tid >= 64) return;
   if (tid == 0) a.path[r.row] = 0;
   w.st.kept = 1;
   w.stand_at(0);
-  int32_t next;
-  w.st.waits = w.walk(next);
-  if (!w.st.waits) w.finish(next);
-  if (!POINTS && tid == 0) a.state[0][s] = w.st;
+  const uint32_t wave = eq_dev::uniform(tid >> 6);
+  if constexpr (!POINTS) {
+    if (few) w.sums = sums;
+  }
+#pragma unroll 1
+  while (true) {
+    if (wave == 0) {
+      int32_t next;
+      w.st.waits = w.walk(next);
+      if (!w.st.waits) w.finish(next);
+      if (!POINTS && w.lane == 0) {
+        if (few) state = w.st;
+        else a.state[0][s] = w.st;
+      }
+    }
+    if (POINTS || !few) return;
+    __syncthreads();
+    w.st = state;
+    if (!w.st.waits) return;
+    if constexpr (!POINTS) {
+#pragma unroll 1
+      for (uint32_t c = wave; c < a.chunks; c += kWalkThreads / 64) {
+        const double v = w.chunk_sum(c, false);
+        if (w.lane == 0) sums[c] = v;
+      }
+      __syncthreads();
+      if (wave == 0) w.st.mass = wave_sum(w.lane < a.chunks ? sums[w.lane] : 0.0);
+    }
+  }
 }
 
 // The rest of a walk.  Pass n: every block of a sequence goes on with the walk by the
@@ -1037,7 +1072,7 @@ void launch_verify(const VerifyArgs &a, uint32_t max_children, hipStream_t strea
     return;
   }
   hipLaunchKernelGGL((walk_kernel<TT, TD, false>), seqs, dim3(kWalkThreads), 0, stream, a);
-  if (a.b.max_new < 2) return;
+  if (a.b.max_new < 2 || a.chunks <= kFewChunks) return;
   // a chain's walk ends with its first rejection
   const uint32_t rounds = max_children == 1 ? 1 : std::min(kRounds, a.b.max_new - 1);
   const dim3 pass((a.chunks + 3) / 4, a.b.n_seqs);
