@@ -690,6 +690,25 @@ struct Walk {
     }
   }
 
+  // Of 256 chunks' sums from c0 on, a lane's four (0 behind the last), in one wait.
+  __device__ __forceinline__ void load4(const double *from, uint32_t c0, double (&v)[4]) const {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) v[j] = from[min(c0 + 64 * j + lane, a.chunks - 1)];
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) v[j] = c0 + 64 * j + lane < a.chunks ? v[j] : 0.0;
+  }
+  // Theirs and all others' sum; v: the first 256's.
+  __device__ __forceinline__ double total_of(const double *from, const double (&v)[4]) const {
+    double sum = ((v[0] + v[1]) + v[2]) + v[3];
+#pragma unroll 1
+    for (uint32_t c0 = 256; c0 < a.chunks; c0 += 256) {
+      double x[4];
+      load4(from, c0, x);
+      sum += ((x[0] + x[1]) + x[2]) + x[3];
+    }
+    return wave_sum(sum);
+  }
+
   // The token behind the path: from what is left of p, or from p where nothing is.
   __device__ __forceinline__ int32_t pick(const Stat &here) {
     const uint32_t chunks = a.chunks;
@@ -700,32 +719,40 @@ struct Walk {
       const Part *const part = a.part + (uint64_t(r.row) + st.cur) * chunks;
       left = chunks <= kLocalChunks ? &tree.weight[0][0] : a.rest + uint64_t(s) * chunks;
 #pragma unroll 1
-      for (uint32_t c = lane; c < chunks; c += 64) {
-        const Part v = part[c];
-        left[c] = v.sum * exp_down(double(v.max) - double(here.max), per_temp) * here.inv;
+      for (uint32_t c0 = lane; c0 < chunks; c0 += 256) {
+        Part v[4];
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) v[j] = part[min(c0 + 64 * j, chunks - 1)];
+#pragma unroll 1
+        for (uint32_t c = c0; c < min(c0 + 256, chunks); c += 64) {
+          left[c] = v[0].sum * exp_down(double(v[0].max) - double(here.max), per_temp) * here.inv;
+#pragma unroll
+          for (uint32_t j = 0; j < 3; ++j) v[j].sum = v[j + 1].sum, v[j].max = v[j + 1].max;
+        }
       }
       __threadfence_block();
       if (hidden) take_out(left);
     }
-    double total = 0.0;
-#pragma unroll 1
-    for (uint32_t c = lane; c < chunks; c += 64) total += left[c];
-    const double limit = random_of(0) * wave_sum(total);
+    double v[4];
+    load4(left, 0, v);
+    const double limit = random_of(0) * total_of(left, v);
     // the first chunk whose running sum passes the limit
     double before = 0.0;
     uint32_t at = chunks;
 #pragma unroll 1
     for (uint32_t c0 = 0; c0 < chunks; c0 += 64) {
-      const double v = c0 + lane < chunks ? left[c0 + lane] : 0.0;
-      const double run = wave_scan(v);
-      const uint64_t m = __ballot(before + run > limit && v > 0.0);
+      if (c0 && c0 % 256 == 0) load4(left, c0, v);
+      const double run = wave_scan(v[0]);
+      const uint64_t m = __ballot(before + run > limit && v[0] > 0.0);
       if (m) {
         const int l = __ffsll((unsigned long long)m) - 1;
         at = c0 + uint32_t(l);
-        before += lane_value(run - v, l);
+        before += lane_value(run - v[0], l);
         break;
       }
       before += lane_value(run, 63);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) v[j] = v[j + 1];
     }
     if (at >= chunks) return here.best;
     if (hidden) hide(at);
@@ -932,13 +959,15 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
   State *const to = a.state[n & 1] + s;
   const bool writer = blockIdx.x == 0;
   const State st = a.state[before][s];
+  const Rows r = rows_of(a.b, s);
   if (!st.waits) {
     if (!END && n && writer && tid == 0) to->waits = 0;
     return;
   }
-  const Rows r = rows_of(a.b, s);
   Walk<TT, TD, false> w(a, tree, s, r, writer, a.sums[before]);
   w.st = st;
+  double v[4];  // the first 256 chunks' sums of the pass before
+  w.load4(w.sums, 0, v);
   double *const new_sums = a.sums[n & 1] + uint64_t(s) * a.chunks;
   auto load_rows = [&](uint32_t i) {
     const uint64_t row = uint64_t(r.row) + i;
@@ -968,10 +997,7 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
   while (true) {
     if (n) {
       if (wave == 0) {
-        double v = 0.0;
-#pragma unroll 1
-        for (uint32_t c = w.lane; c < a.chunks; c += 64) v += w.sums[c];
-        w.st.mass = wave_sum(v);
+        w.st.mass = w.total_of(w.sums, v);
         int32_t next;
         w.st.waits = w.walk(next);
         if (!w.st.waits) w.finish(next);
@@ -990,6 +1016,7 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
     }
     pass(wave, kWalkThreads / 64, w.sums);
     __syncthreads();
+    w.load4(w.sums, 0, v);
   }
 }
 
