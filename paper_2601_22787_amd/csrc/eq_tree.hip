@@ -64,7 +64,7 @@ struct MaskArgs {
 };
 
 // A block for a sequence, a thread for a node, which walks up through the parents in
-// LDS: as many steps as the node is deep.  64 trees of up to 60 nodes 3.5 us, one launch
+// LDS: as many steps as the node is deep.  64 trees of up to 60 nodes 3.7 us, one launch
 // and its chain of loads.
 __global__ __launch_bounds__(kMaxNodes) void tree_mask_kernel(MaskArgs a) {
   __shared__ int32_t up[kMaxNodes];
@@ -947,7 +947,7 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
 //
 // Passes by all compute units take 5.3 us for 8 sequences of 100003 logits, 8 for 32 of
 // 131072; by one block about 13.  Four of them in launches of their own: 8 trees of up
-// to 32 nodes 58.8 us in the mean of 8 inputs (three 61.3, five 60.7, eight 67.5); an
+// to 32 nodes 57.9 us in the mean of 8 inputs (three 60.4, five 59.7, eight 65.9); an
 // idle one is 1 to 2 us.  A counter and the last block to arrive in place of the next
 // launch: its fences took longer (36 us for 1024 blocks).
 template <typename TT, typename TD, bool END>
