@@ -135,7 +135,7 @@ constexpr uint32_t kNone = 0xFFFF;
 constexpr double kLeast = 0x1p-32;  // of p: less is taken for nothing
 constexpr uint32_t kRounds = 4;
 constexpr uint32_t kLocalChunks = 1024;  // chunks whose sums a block keeps in LDS
-constexpr uint32_t kStatWaves = 3072, kMostPer = 3;
+constexpr uint32_t kStatWaves = 3 * 1024, kMostPer = 3;  // (three for each SIMD)
 
 struct VerifyArgs {
   BatchArgs b;
