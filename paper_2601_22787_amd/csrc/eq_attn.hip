@@ -138,20 +138,26 @@ __device__ inline int32_t wave_max(int32_t x) {
   return x;
 }
 
-// Sums of the lanes up to each.
-__device__ inline uint32_t wave_scan(uint32_t x, uint32_t lane) {
-#pragma unroll
-  for (uint32_t d = 1; d < 64; d *= 2) {
-    const uint32_t o = uint32_t(__shfl_up(int(x), d));
-    x += lane >= d ? o : 0u;
-  }
+// v of the lane that CTRL names, 0 where there is none or the row is not in ROWS.
+template <int CTRL, int ROWS, typename T>
+__device__ inline T from_lane(T v) {
+  return __builtin_bit_cast(
+      T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xF, true));
+}
+// Sums of the lanes up to each: within rows of 16, then from row to row.
+template <typename T>
+__device__ inline T wave_scan(T x) {
+  x += from_lane<0x111, 0xF>(x);
+  x += from_lane<0x112, 0xF>(x);
+  x += from_lane<0x114, 0xF>(x);
+  x += from_lane<0x118, 0xF>(x);
+  x += from_lane<0x142, 0xA>(x);  // row_bcast:15
+  x += from_lane<0x143, 0xC>(x);  // row_bcast:31
   return x;
 }
 template <typename T>
 __device__ inline T wave_sum(T x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-  return x;
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x)), 63));
 }
 
 // What block `number` of a head does for a batch of trees, up to 64 of them: the host
@@ -175,13 +181,13 @@ __device__ inline Share even_share(const AttnArgs &a, uint32_t number) {
     tiles = max((uint32_t(q.len) + kPromptTile - 1) / kPromptTile, first) - first;
     q_tiles = (uint32_t(q.count) * a.group + kPromptCols - 1) / kPromptCols;
   }
-  const uint32_t run = max(2 * kFillBlocks / w.kv_heads, 1u);  // blocks of a head
+  const uint32_t run = head_blocks(w.kv_heads);
   // (a product may pass 32 bits; a chunk of 2^24 tiles is any sequence whole)
   const float even = ceilf(wave_sum(float(q_tiles) * float(tiles)) / float(run));
   uint32_t ct = max(a.chunk_tiles, uint32_t(fminf(even, 0x1p24f)));
   auto blocks = [&]() { return max((tiles + ct - 1) / ct, 1u) * q_tiles; };
-  for (int i = 0; i < 12 && wave_sum(blocks()) > run; ++i) ct += (ct + 15) / 16;
-  const uint32_t mine = blocks(), end = wave_scan(mine, lane);
+  for (int i = 0; i < 24 && wave_sum(blocks()) > run; ++i) ct += (ct + 31) / 32;
+  const uint32_t mine = blocks(), end = wave_scan(mine);
   const uint64_t m = __ballot(number < end);
   Share r{0, 0, 0, ct, m != 0};
   if (!m) return r;
@@ -1114,9 +1120,9 @@ __global__ __launch_bounds__(2 * D) void join_kernel(AttnArgs a) {
   const uint32_t token = blockIdx.x / heads, head = blockIdx.x % heads;
   const Seq q = sequence(w, s);
   if (int32_t(token) >= q.count) return;
-  if (TREE && a.even) a.chunk_tiles = *a.even;
   const uint32_t h = head / a.group, index = token * a.group + head % a.group;
   const uint32_t qt = index / COLS;
+  if (TREE && a.even) a.chunk_tiles = *a.even;
   const Span sp = span_of<COLS, TILE, TREE>(a, q, qt * COLS);
   if (sp.chunks <= 1) return;
   const uint64_t first =
@@ -1187,9 +1193,9 @@ __global__ __launch_bounds__(256) void join_rows_kernel(AttnArgs a) {
   const uint32_t token = at / heads, head = at % heads;
   const Seq q = sequence(w, s);
   if (token >= uint32_t(q.count)) return;
-  if (a.even) a.chunk_tiles = *a.even;
   const uint32_t h = head / a.group, index = token * a.group + head % a.group;
   const uint32_t qt = index / kPromptCols;
+  if (a.even) a.chunk_tiles = *a.even;
   const Span sp = span_of<kPromptCols, kPromptTile, true>(a, q, qt * kPromptCols);
   if (sp.chunks <= 1) return;
   const uint64_t first = (((uint64_t(s) * w.kv_heads + h) * a.q_tiles + qt) * a.chunks) * kPromptCols +
@@ -1290,19 +1296,20 @@ bool heads_ok(const eq_kv_cache *c, uint32_t q_heads) {
 
 // The columns of all heads are counted in 32 bits, and one launch takes them.  (A
 // window leaves fewer chunks, and chunks are joined where there are few columns.)
-bool size_ok(const eq_kv_cache *c, const eq_kv_batch *b, uint32_t q_heads) {
+bool size_ok(const eq_kv_cache *c, const eq_kv_batch *b, uint32_t q_heads, bool tree) {
   if (uint64_t(b->max_new) * q_heads > 0x7FFFFFFFu) return false;
-  const Plan p = plan_attn(b->n_seqs, c->kv_heads, q_heads / c->kv_heads, b->max_new, b->max_len, 0);
+  const Plan p =
+      plan_attn(b->n_seqs, c->kv_heads, q_heads / c->kv_heads, b->max_new, b->max_len, 0, tree);
   return uint64_t(c->kv_heads) * p.q_tiles * p.chunks <= kMaxBlocks;
 }
 
 template <bool TREE>
 size_t workspace_bytes(const eq_kv_cache *cache, const eq_kv_batch *batch, uint32_t q_heads) {
   if (!batch_ok(cache, batch) || !heads_ok(cache, q_heads) || batch->n_seqs == 0 ||
-      batch->max_new == 0 || !size_ok(cache, batch, q_heads))
+      batch->max_new == 0 || !size_ok(cache, batch, q_heads, TREE))
     return 0;
   return attn_bytes<TREE>(plan_attn(batch->n_seqs, cache->kv_heads, q_heads / cache->kv_heads,
-                                    batch->max_new, batch->max_len, 0),
+                                    batch->max_new, batch->max_len, 0, TREE),
                           cache, batch);
 }
 
@@ -1320,9 +1327,9 @@ int attention(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t
     return EQ_EINVAL;
   if (TREE && (!mask || (window && !positions))) return EQ_EINVAL;
   const uint32_t group = q_heads / cache->kv_heads;
-  if (!size_ok(cache, batch, q_heads)) return EQ_EINVAL;
+  if (!size_ok(cache, batch, q_heads, TREE)) return EQ_EINVAL;
   const Plan p = plan_attn(batch->n_seqs, cache->kv_heads, group, batch->max_new, batch->max_len,
-                           window);
+                           window, TREE);
   const size_t need = attn_bytes<TREE>(p, cache, batch);
   if (need && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15))) return EQ_EINVAL;
   AttnArgs a{view(cache, batch), q, q_stride, out, static_cast<float *>(ws), nullptr, group, window,
@@ -1330,9 +1337,12 @@ int attention(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t
              (batch->max_new + 31) / 32, nullptr};
   if (need)
     a.stat = reinterpret_cast<float2 *>(a.part + part_cols(p, cache, batch) * cache->head_dim);
-  if (TREE && need && p.prompt && batch->n_seqs <= 64)
+  if (TREE && need && p.prompt && batch->n_seqs <= kShareSeqs)
     a.even = reinterpret_cast<uint32_t *>(a.stat + part_cols(p, cache, batch));
-  const dim3 grid(cache->kv_heads * p.q_tiles * p.chunks, batch->n_seqs);
+  dim3 grid(cache->kv_heads * p.q_tiles * p.chunks, batch->n_seqs);
+  if (a.even)  // each sequence's last chunks beside what runs at once, and a rounding
+    grid = dim3(cache->kv_heads * std::min(head_blocks(cache->kv_heads) + batch->n_seqs * p.q_tiles + 1,
+                                           batch->n_seqs * p.q_tiles * p.chunks));
   const dim3 join(batch->max_new * q_heads, batch->n_seqs);
   // a tile in one page has one page number to read and take addresses from (284 000
   // tokens: 61.9 us, as four 62.8)

@@ -43,9 +43,21 @@ struct Plan {
 constexpr uint32_t kFewCols = 64, kFillBlocks = 256, kLongTokens = 8192;
 // attn_kernel: tiles of one chunk, and with half the card's blocks or more
 constexpr uint32_t kWholeTiles = 16, kWholeFilled = 32;
+// prompt_kernel for trees: the batches whose chunks the device sets from all lengths, a
+// sequence for a lane; the blocks of most chunks; and a head's blocks that run at once.
+// Those chunks are there for batches of more blocks too, up to half of the most, where
+// long sequences may be among short ones.  Sequences x nodes, 64 heads on 8, up to so
+// many tokens: us whole / in chunks
+//   ragged: 16 x 20, 16384: 318 / 76    16 x 64, 9000: 190 / 101   32 x 16, 32768: 637 / 306
+//           10 x 33, 8200: 69.5 / 69.0  40 x 20, 8192: 258 / 161   32 x 64, 9000: 302 / 266
+//   alike:  8 x 64, 16384: 326 / 274    12 x 64, 9000: 257 / 265   32 x 64, 9000: 560 / 575
+constexpr uint32_t kShareSeqs = 64, kTreeBlocks = 2048;
+constexpr uint32_t head_blocks(uint32_t kv_heads) {
+  return std::max(2 * kFillBlocks / kv_heads, 1u);
+}
 
 inline Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32_t max_new,
-                      uint32_t max_len, uint32_t window) {
+                      uint32_t max_len, uint32_t window, bool tree = false) {
   Plan p;
   const uint64_t cols = uint64_t(max_new) * group;
   const uint64_t prompts = uint64_t(n_seqs) * kv_heads * ((cols + kPromptCols - 1) / kPromptCols);
@@ -62,6 +74,9 @@ inline Plan plan_attn(uint32_t n_seqs, uint32_t kv_heads, uint32_t group, uint32
   auto round4 = [](uint64_t v) { return uint32_t(std::max<uint64_t>((v + 3) / 4 * 4, 4)); };
   uint32_t ct = round4((tiles + want - 1) / want);
   if (!whole && work < 2048) ct = std::min(ct, (p.prompt ? 2048 : 4096) / p.tile);
+  if (tree && p.prompt && n_seqs <= kShareSeqs && work >= kFillBlocks && 2 * work <= kTreeBlocks &&
+      max_len >= kLongTokens)
+    ct = std::max(round4((uint64_t(tiles) * work + kTreeBlocks - 1) / kTreeBlocks), 2048 / p.tile);
   p.chunks = std::max((tiles + ct - 1) / ct, 1u);
   ct = round4((tiles + p.chunks - 1) / p.chunks);  // chunks of one length
   // a window leaves fewer tiles (a query's window and the others' of its

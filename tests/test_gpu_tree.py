@@ -164,6 +164,21 @@ def test_attention(eq, news, lens, hq, hk, dim, page, window, bound):
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
 
 
+# more columns than the card runs at once: chunks by the lengths of all (65 sequences: none)
+MANY = [
+    ([130, 70, 129], [5000, 300, 2500], 64, 64, 64, 128, 0),
+    ([130, 0, 129], [3100, 0, 130], 64, 64, 64, 32, 0),
+    ([130, 70, 129], [5000, 300, 2500], 64, 64, 64, 64, 4000),
+    ([9] * 32, [9, 4200] + [40] * 30, 64, 8, 128, 64, 0),
+    ([66] + [1] * 64, [2300] + [3] * 64, 4, 4, 64, 32, 0),
+]
+
+
+@pytest.mark.parametrize("news,lens,hq,hk,dim,page,window", MANY)
+def test_attention_of_many(eq, news, lens, hq, hk, dim, page, window):
+    test_attention(eq, news, lens, hq, hk, dim, page, window, 8192)
+
+
 @pytest.mark.parametrize("bound", [0, 8192])
 @pytest.mark.parametrize("news,lens,hq,hk,dim,page", [c[:6] for c in CASES])
 def test_a_chain_is_causal_attention(eq, news, lens, hq, hk, dim, page, bound):
