@@ -465,7 +465,8 @@ size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, 
  * none is, the token behind the path is the first at which the running sum of what is
  * left of p, in the tokens' order, passes random[row of node 0] times the whole.  Where
  * less than 2^-32 of p is left, no further child is tested and that token is of p
- * itself.  random: fp32, taken into [0, 1 - 2^-24] (NaN: 0).
+ * itself.  Where less than 2^-900 of q is left, no further child is tested.
+ * random: fp32, taken into [0, 1 - 2^-24] (NaN: 0).
  * A temperature that is not above 0: the child that is the target's largest logit is
  * accepted, the lowest of equal ones; random and draft are not looked at.
  * path: the kept nodes of each sequence from its first row on, node 0 first, then -1;

@@ -5,12 +5,14 @@
 // r_0 = p, the children x_1, x_2, .. of a node are tested in order: x_j is accepted
 // with probability min(1, r(x_j) / q(x_j)), else r becomes max(r - q, 0) and q loses
 // x_j, both normalised again.  All of that is one family of functions,
-//   r ~ max(p - t q, 0),  G(t) = sum max(p - t q, 0),  Q = 1 - sum of the rejected q,
+//   r ~ max(p - t q, 0),  G(t) = sum max(p - t q, 0),  Q = sum of the q not rejected,
 // from t = 0 (G = 1, Q = 1), with t + G / Q in the place of t after a rejection:
 //   max(p - t q, 0) / G - q / Q = (max(p - t q, 0) - (G / Q) q) / G.
 // A rejected x has p(x) < t q(x) from then on, so that q need not be cut there.  x is
 // accepted when u G q(x) < max(p(x) - t q(x), 0) Q.  A rejection thus costs one pass
-// over the vocabulary for one number.
+// over the vocabulary for G, and for Q where another child is there.  (Q is no 1 - q: a
+// draft that is sure of a token leaves 2^-40 and less, of which the difference, off by
+// 2^-38, holds nothing; and a target that rejects the token comes here often.)
 //
 // Everything is in 64 bits.  A token is where a running sum of probabilities passes u
 // times the whole: the sum's error, over the probabilities near it, is how often a
@@ -120,9 +122,11 @@ struct Stat {
 // Where a sequence's walk stands: at node `cur`, whose children before `child` have been
 // rejected.
 struct State {
-  double t, mass, left;  // mass: G(t), or what the rejected points have left of p
+  double t, mass, left;  // mass: G(t), or what the rejected points have left of p; left: Q
   uint32_t cur, child, kept;
-  uint32_t waits;        // for the sums of max(p - t q, 0)
+  uint32_t waits;        // for the sums of max(p - t q, 0): 1; of the q too: 2
+  uint32_t out;          // different tokens among the rejected children of `cur`
+  int32_t token;         // the last of them
 };
 
 // A node's place among the others.
@@ -133,6 +137,10 @@ struct Link {
 constexpr uint32_t kNone = 0xFFFF;
 
 constexpr double kLeast = 0x1p-32;  // of p: less is taken for nothing
+// Of q: with less left no further child is tested.  Above it no product here leaves the
+// range of numbers, nor does a q that counts; the token is then of what is left of p,
+// which is the target's distribution whatever was not tested.
+constexpr double kLeastDraft = 0x1p-900;
 constexpr uint32_t kRounds = 4;
 constexpr uint32_t kLocalChunks = 1024;  // chunks whose sums a block keeps in LDS
 constexpr uint32_t kStatWaves = 3 * 1024, kMostPer = 3;  // (three for each SIMD)
@@ -147,7 +155,8 @@ struct VerifyArgs {
   // workspace
   Part *part;                      // [n_tokens][chunks], of the target's rows
   Part *target_group, *draft_group;  // [n_tokens][groups], `per` chunks of 4 wavefronts each
-  double *sums[2];                 // [n_seqs][chunks], of even and odd passes
+  double *sums[2];                 // [n_seqs][2][chunks], of even and odd passes: of
+                                   // max(p - t q, 0), and of the q not rejected
   double *rest;                    // [n_seqs][chunks], where those are more than kLocalChunks
   double *px, *qx;                 // [n_tokens]
   Stat *target_stat, *draft_stat;  // [n_tokens]
@@ -567,7 +576,7 @@ struct Walk {
   __device__ inline Walk(const VerifyArgs &args, Tree &t, uint32_t seq, const Rows &rows, bool writer,
                          double *chunk_sums)
       : a(args), tree(t), r(rows), s(seq), count(uint32_t(rows.count)), lane(threadIdx.x & 63),
-        writes(writer), sums(POINTS ? nullptr : chunk_sums + uint64_t(seq) * args.chunks) {
+        writes(writer), sums(POINTS ? nullptr : chunk_sums + 2 * uint64_t(seq) * args.chunks) {
     const float temp = temperature_of(a, s);
     greedy = !(temp > 0.0f);
     per_temp = per_temperature(temp);
@@ -590,6 +599,7 @@ struct Walk {
   __device__ inline void stand_at(uint32_t node) {
     st.cur = node, st.child = tree.link[node].first;
     st.t = 0.0, st.mass = 1.0, st.left = 1.0;
+    st.out = 0, st.token = 0;
   }
   __device__ inline void go_down(uint32_t c) {
     if (writes && lane == 0) a.path[r.row + int32_t(st.kept)] = int32_t(c);
@@ -625,44 +635,87 @@ struct Walk {
     }
   }
 
-  // the sum of a chunk's weights; hidden: without the tokens in tree.hidden
-  __device__ __forceinline__ double chunk_sum(uint32_t chunk, bool hidden) const {
+  // the sum of a chunk's weights without the tokens in tree.hidden
+  __device__ __forceinline__ double chunk_sum(uint32_t chunk) const {
     float p[16], q[16] = {};
     load(chunk * kChunk + 4 * lane, 256, (chunk + 1) * kChunk > a.vocab, p, q);
     double sum = 0.0;
     weights(p, q, [&](int i, double (&w)[4]) {
-      if (POINTS && hidden) {
-        const uint32_t at = 256 * uint32_t(i) + 4 * lane, bits = tree.hidden[at / 32] >> (at % 32);
+      const uint32_t at = 256 * uint32_t(i) + 4 * lane, bits = tree.hidden[at / 32] >> (at % 32);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = bits >> e & 1 ? 0.0 : w[e];
-      }
+      for (int e = 0; e < 4; ++e) w[e] = bits >> e & 1 ? 0.0 : w[e];
       sum += (w[0] + w[1]) + (w[2] + w[3]);
     });
     return wave_sum(sum);
   }
 
-  // Tests children and goes down until the sums of what is left are needed (true) or
-  // the walk has ended at `next` (false).
-  __device__ __forceinline__ bool walk(int32_t &next) {
+  // Which of a lane's 16 tokens of a chunk (as load16's, with step 256) are rejected
+  // children's.  One of them is known without the tree.
+  __device__ inline uint32_t rejected(uint32_t chunk) const {
+    const auto bit = [&](uint32_t token) {
+      const uint32_t at = token % kChunk;
+      return at % 256 / 4 == lane ? 1u << (at / 256 * 4 + at % 4) : 0u;
+    };
+    if (st.out == 1) return uint32_t(st.token) / kChunk == chunk ? bit(uint32_t(st.token)) : 0u;
+    uint32_t bits = 0;
+#pragma unroll 1
+    for (uint32_t j0 = 0; j0 < st.child; j0 += 64) {
+      const uint32_t j = j0 + lane;
+      uint64_t m = __ballot(j < st.child && gone(j) && chunk_of(j) == chunk);
+      for (; m; m &= m - 1) bits |= bit(uint32_t(tree.token[j0 + uint32_t(__ffsll((unsigned long long)m)) - 1]));
+    }
+    return bits;
+  }
+
+  // The sums that the walk waits for, of a chunk.
+  __device__ __forceinline__ void pass(uint32_t chunk, double *out) const {
+    const bool both = st.waits > 1;
+    const uint32_t without = both ? rejected(chunk) : 0;
+    float p[16], q[16] = {};
+    load(chunk * kChunk + 4 * lane, 256, (chunk + 1) * kChunk > a.vocab, p, q);
+    const Stat ps = tree.target[st.cur], qs = tree.draft[st.cur];
+    double sum = 0.0, rest = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i, next<4>(p), next<4>(q)) {
+      double w[4], v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = prob(qs, q[e]);
+        w[e] = fmax(__builtin_fma(-st.t, v[e], prob(ps, p[e])), 0.0);
+        v[e] = without >> (4 * i + e) & 1 ? 0.0 : v[e];
+      }
+      sum += (w[0] + w[1]) + (w[2] + w[3]);
+      rest += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) out[chunk] = sum;
+    if (!both) return;
+    rest = wave_sum(rest);
+    if (lane == 0) out[a.chunks + chunk] = rest;
+  }
+
+  // Tests children and goes down until sums are needed (what st.waits says) or the walk
+  // has ended at `next` (0).
+  __device__ __forceinline__ uint32_t walk(int32_t &next) {
     next = -1;
 #pragma unroll 1
     while (true) {
       const Stat here = tree.target[st.cur];
-      if (here.best < 0) return false;
+      if (here.best < 0) return 0;
       uint32_t c = st.child;
       if (greedy) {
         while (c != kNone && tree.token[c] != here.best) c = tree.link[c].next;
         if (c == kNone) {
           next = here.best;
-          return false;
+          return 0;
         }
         go_down(c);
         continue;
       }
-      if (!POINTS && c != kNone && tree.draft[st.cur].best < 0) return false;
+      if (!POINTS && c != kNone && tree.draft[st.cur].best < 0) return 0;
       bool down = false;
 #pragma unroll 1
-      while (c != kNone && st.mass >= kLeast) {
+      while (c != kNone && st.mass >= kLeast && st.left >= kLeastDraft) {
         const Link link = tree.link[c];
         const double u = random_of(c), p = tree.px[c], q = POINTS ? 0.0 : tree.qx[c];
         st.child = link.next;
@@ -675,16 +728,17 @@ struct Walk {
           if constexpr (POINTS) {
             st.mass = fmax(st.mass - rest, 0.0);
           } else {
-            if (st.left > 0.0) st.t += st.mass / st.left;
-            if (!a.replace && !link.again) st.left = fmax(st.left - q, 0.0);
-            return true;
+            st.t += st.mass / st.left;
+            if (link.again) return 1;
+            ++st.out, st.token = tree.token[c];
+            return !a.replace && st.child != kNone ? 2 : 1;
           }
         }
         c = link.next;
       }
       if (!down) {
         if (writes) next = pick(here);
-        return false;
+        return 0;
       }
       go_down(c);
     }
@@ -786,7 +840,8 @@ struct Walk {
     return int32_t(at * kChunk) + 16 * l + e;
   }
 
-  // A child of `cur` whose token was rejected, the first of that token.
+  // A child of `cur` with a token, the first of that token: a rejected one, among those
+  // that have been tested.
   __device__ inline bool gone(uint32_t j) const {
     return j < count && tree.up[j] == int32_t(st.cur) && !outside(j) && !tree.link[j].again;
   }
@@ -817,7 +872,7 @@ struct Walk {
         double rest = all - wave_sum(out);
         if (!(rest > all * 0x1p-20)) {
           hide(chunk);
-          rest = chunk_sum(chunk, true);
+          rest = chunk_sum(chunk);
         }
         if (lane == 0) left[chunk] = rest;
       }
@@ -860,7 +915,7 @@ template <typename TT, typename TD, bool POINTS>
 __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
   __shared__ Tree tree;
   __shared__ State state;
-  __shared__ double sums[kFewChunks];
+  __shared__ double sums[2 * kFewChunks];
   const uint32_t s = blockIdx.x, tid = threadIdx.x;
   const Rows r = rows_of(a.b, s);
   if (r.count <= 0) {
@@ -930,12 +985,12 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
     if (!w.st.waits) return;
     if constexpr (!POINTS) {
 #pragma unroll 1
-      for (uint32_t c = wave; c < a.chunks; c += kWalkThreads / 64) {
-        const double v = w.chunk_sum(c, false);
-        if (w.lane == 0) sums[c] = v;
-      }
+      for (uint32_t c = wave; c < a.chunks; c += kWalkThreads / 64) w.pass(c, sums);
       __syncthreads();
-      if (wave == 0) w.st.mass = wave_sum(w.lane < a.chunks ? sums[w.lane] : 0.0);
+      if (wave == 0) {
+        w.st.mass = wave_sum(w.lane < a.chunks ? sums[w.lane] : 0.0);
+        if (w.st.waits > 1) w.st.left = wave_sum(w.lane < a.chunks ? sums[a.chunks + w.lane] : 0.0);
+      }
     }
   }
 }
@@ -966,19 +1021,17 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
   }
   Walk<TT, TD, false> w(a, tree, s, r, writer, a.sums[before]);
   w.st = st;
-  double v[4];  // the first 256 chunks' sums of the pass before
+  double v[4], left[4];  // the first 256 chunks' sums of the pass before
   w.load4(w.sums, 0, v);
-  double *const new_sums = a.sums[n & 1] + uint64_t(s) * a.chunks;
+  w.load4(w.sums + a.chunks, 0, left);  // (of anything, if they were not wanted)
+  double *const new_sums = a.sums[n & 1] + 2 * uint64_t(s) * a.chunks;
   auto load_rows = [&](uint32_t i) {
     const uint64_t row = uint64_t(r.row) + i;
     tree.target[i] = a.target_stat[row], tree.draft[i] = a.draft_stat[row];
   };
   auto pass = [&](uint32_t first, uint32_t step, double *out) {
 #pragma unroll 1
-    for (uint32_t c = first; c < a.chunks; c += step) {
-      const double v = w.chunk_sum(c, false);
-      if (w.lane == 0) out[c] = v;
-    }
+    for (uint32_t c = first; c < a.chunks; c += step) w.pass(c, out);
   };
   if (n == 0) {  // (the walk waits already)
     if (tid == 0) load_rows(st.cur);
@@ -998,6 +1051,7 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
     if (n) {
       if (wave == 0) {
         w.st.mass = w.total_of(w.sums, v);
+        if (w.st.waits > 1) w.st.left = w.total_of(w.sums + a.chunks, left);
         int32_t next;
         w.st.waits = w.walk(next);
         if (!w.st.waits) w.finish(next);
@@ -1017,6 +1071,7 @@ __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyAr
     pass(wave, kWalkThreads / 64, w.sums);
     __syncthreads();
     w.load4(w.sums, 0, v);
+    w.load4(w.sums + a.chunks, 0, left);
   }
 }
 
@@ -1073,8 +1128,8 @@ size_t lay_out(VerifyArgs &a, bool draft, void *ws) {
   a.target_group = room.take<Part>(rows * a.groups);
   if (a.chunks > kLocalChunks) a.rest = room.take<double>(seqs * a.chunks);
   if (draft) {
-    a.sums[0] = room.take<double>(seqs * a.chunks);
-    a.sums[1] = room.take<double>(seqs * a.chunks);
+    a.sums[0] = room.take<double>(2 * seqs * a.chunks);
+    a.sums[1] = room.take<double>(2 * seqs * a.chunks);
     a.state[0] = room.take<State>(seqs);
     a.state[1] = room.take<State>(seqs);
     a.draft_group = room.take<Part>(rows * a.groups);
