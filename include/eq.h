@@ -440,8 +440,8 @@ size_t eq_attn_kv4_tree_workspace_bytes(const eq_kv_cache *cache, const eq_kv_ba
  * sequence's new ones, with window > 0 those at places above positions[row] - window
  * (positions below the first new place count as that; NULL without a window), and of
  * the new ones those of its bits (mask: [n_tokens][W] as above; any bits, not a tree's
- * alone; the window is not looked at for them).  A row without any bit sees nothing:
- * zeros.  Types, precision, alignment and workspace as for eq_attn_kv4. */
+ * alone; the window is not looked at for them; bits behind the sequence's rows, of which
+ * max_new count, stand for no token).  A row without any bit sees nothing: zeros.  Types, precision, alignment and workspace as for eq_attn_kv4. */
 int eq_attn_kv4_tree(const eq_kv_cache *cache, const eq_kv_batch *batch, const uint16_t *q,
                      uint64_t q_stride, uint32_t q_heads, float scale, uint32_t window,
                      const uint32_t *mask, const int32_t *positions, uint16_t *out, void *ws,

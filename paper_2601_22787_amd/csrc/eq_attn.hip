@@ -71,17 +71,29 @@ __device__ inline int32_t start_of(uint32_t window, int32_t pos) {
 }
 
 // TREE: all columns see the tokens before the new ones (what a window hides of them
-// and lanes without a node are the kernels' own), and new ones by their masks.
+// and lanes without a node are the kernels' own), and new ones by their masks, those of
+// the rows that count: what is behind them would be more than the host has chunks for.
+struct Tiles {
+  uint32_t seen, first, last;
+};
+template <uint32_t TILE>
+__device__ inline Tiles tree_tiles(uint32_t window, const Seq &q) {
+  Tiles t;
+  t.seen = uint32_t(min(max(q.base + q.count, 0), q.len));
+  t.first = uint32_t(start_of(window, max(q.base, 0))) / TILE;
+  t.last = max((t.seen + TILE - 1) / TILE, t.first);
+  return t;
+}
+
 template <uint32_t COLS, uint32_t TILE, bool TREE>
 __device__ inline Span span_of(const AttnArgs &a, const Seq &q, uint32_t col0) {
   Span p{};
   p.cols = uint32_t(q.count) * a.group;
   if (col0 >= p.cols) return p;
   if constexpr (TREE) {
+    const Tiles t = tree_tiles<TILE>(a.window, q);
     p.hi_min = min(max(q.base, 0), q.len);
-    p.seen = uint32_t(q.len);
-    p.first = uint32_t(start_of(a.window, max(q.base, 0))) / TILE;
-    p.last = max((p.seen + TILE - 1) / TILE, p.first);
+    p.seen = t.seen, p.first = t.first, p.last = t.last;
     p.chunks = min((p.last - p.first + a.chunk_tiles - 1) / a.chunk_tiles, a.chunks);
     return p;
   }
@@ -177,15 +189,16 @@ __device__ inline Share even_share(const AttnArgs &a, uint32_t number) {
   uint32_t tiles = 0, q_tiles = 0;
   if (lane < w.n_seqs) {
     const Seq q = sequence(w, lane);
-    const uint32_t first = uint32_t(start_of(a.window, max(q.base, 0))) / kPromptTile;
-    tiles = max((uint32_t(q.len) + kPromptTile - 1) / kPromptTile, first) - first;
+    const Tiles t = tree_tiles<kPromptTile>(a.window, q);
+    tiles = t.last - t.first;
     q_tiles = (uint32_t(q.count) * a.group + kPromptCols - 1) / kPromptCols;
   }
   const uint32_t run = head_blocks(w.kv_heads);
   // (a product may pass 32 bits; a chunk of 2^24 tiles is any sequence whole)
   const float even = ceilf(wave_sum(float(q_tiles) * float(tiles)) / float(run));
   uint32_t ct = max(a.chunk_tiles, uint32_t(fminf(even, 0x1p24f)));
-  auto blocks = [&]() { return max((tiles + ct - 1) / ct, 1u) * q_tiles; };
+  // (as span_of counts them)
+  auto blocks = [&]() { return max(min((tiles + ct - 1) / ct, a.chunks), 1u) * q_tiles; };
   for (int i = 0; i < 24 && wave_sum(blocks()) > run; ++i) ct += (ct + 31) / 32;
   const uint32_t mine = blocks(), end = wave_scan(mine);
   const uint64_t m = __ballot(number < end);
