@@ -491,9 +491,9 @@ int eq_tree_verify(const eq_kv_batch *batch, const int32_t *parents, const int32
  * places takes the key and value of new token path[seq_start[s] + k], for k < kept[s].
  * Entries below k or beyond the sequence's rows, and tokens of pages that are not
  * there, are left out.  Places behind the kept ones hold what they held.  new_len (or
- * NULL): int32 [n_seqs], kv_len less the nodes that were not kept, in memory of its
- * own (not kv_len's or kept's, which other blocks read).  Two sequences may share pages, but not 8 aligned positions
- * that either moves tokens to. */
+ * NULL): int32 [n_seqs], kv_len less the nodes that were not kept (0 where that is below
+ * it), in memory of its own (not kv_len's or kept's, which other blocks read).  Two
+ * sequences may share pages, but not 8 aligned positions that either moves tokens to. */
 #define EQ_KEEP_CACHES 128
 int eq_kv_keep(const eq_kv_cache *const *caches, uint32_t n, const eq_kv_batch *batch,
                const int32_t *path, const int32_t *kept, int32_t *new_len, hipStream_t stream);

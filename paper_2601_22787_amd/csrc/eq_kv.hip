@@ -468,7 +468,7 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
   const Seq q = sequence(w, s);
   const int32_t kept = min(max(a.kept[s], 0), q.count);
   if (a.new_len && blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0)
-    a.new_len[s] = q.count > 0 ? max(q.base, 0) + kept : max(w.kv_len[s], 0);
+    a.new_len[s] = max(q.count > 0 ? q.base + kept : w.kv_len[s], 0);
   if (h >= w.kv_heads || kept <= 0) return;
   const uint32_t t = lane >> 3, sub = lane & 7;
   const uint32_t page_mask = (1u << w.page_shift) - 1;
