@@ -474,8 +474,10 @@ size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, 
  * them, or -1 where a row of logits that is looked at holds a NaN or +infinity or
  * nothing above -infinity (the path up to there is kept).  Tokens outside the
  * vocabulary are never accepted, nor nodes that are not their parent's later rows.
- * All in 64 bits: tokens are those of exact arithmetic but where a random number is
- * within about 2^-36 of a border.  max_children bounds a node's children (1: a
+ * All in 64 bits, probabilities to 2^-37.8 of themselves: tokens are those of exact
+ * arithmetic but where a random number is within about 2^-35 over what is left of p of a
+ * border.  (What is left is a difference of rounded numbers; it comes that far in its
+ * part of all cases, so that about 2^-35 of them are concerned.)  max_children bounds a node's children (1: a
  * chain); with more than that, results are the same, and slower.  vocab is at most
  * 2^24.  ws/ws_bytes: at least eq_tree_verify_workspace_bytes(), 16-byte aligned;
  * nothing in it is kept between calls. */
