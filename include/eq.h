@@ -477,7 +477,9 @@ size_t eq_tree_verify_workspace_bytes(const eq_kv_batch *batch, uint32_t vocab, 
  * All in 64 bits, probabilities to 2^-37.8 of themselves: tokens are those of exact
  * arithmetic but where a random number is within about 2^-35 over what is left of p of a
  * border.  (What is left is a difference of rounded numbers; it comes that far in its
- * part of all cases, so that about 2^-35 of them are concerned.)  max_children bounds a node's children (1: a
+ * part of all cases, so that about 2^-35 of them are concerned.)  The order of sums
+ * depends on n_tokens, vocab and draft alone: the same call gives the same tokens, and so
+ * near a border a sequence may have another one beside others than alone.  max_children bounds a node's children (1: a
  * chain); with more than that, results are the same, and slower.  vocab is at most
  * 2^24.  ws/ws_bytes: at least eq_tree_verify_workspace_bytes(), 16-byte aligned;
  * nothing in it is kept between calls. */

@@ -1118,7 +1118,9 @@ struct Room {
   }
 };
 
-// Splits a batch's rows and a workspace for them; the bytes that it needs.
+// Splits a batch's rows and a workspace for them; the bytes that it needs.  (`per` goes by
+// the whole batch's size, so the order of a row's sums and its exponentials' references do
+// too: statistics of the same row may differ by 2^-38 between batches.)
 size_t lay_out(VerifyArgs &a, bool draft, void *ws) {
   a.chunks = (a.vocab + kChunk - 1) / kChunk;
   const uint64_t work = uint64_t(a.chunks) * a.b.n_tokens * (draft ? 2 : 1);
