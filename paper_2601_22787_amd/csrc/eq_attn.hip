@@ -390,10 +390,12 @@ __device__ inline int4v load_codes(const uint8_t *p) {
 // join.
 //
 // TREE: a column's new tokens are its mask's, 16 bits of it for 16 tokens in a row.
-// Here 16 columns see a tile of 128 tokens, and the 460 vector instructions of that are
-// the limit: eight trees of 16 nodes, 64 heads on 8, 4096 tokens in 27 us, vector units
-// 0.4 and matrix units 0.2 busy over the whole launch, 8 wavefronts a compute unit at
-// most.  A form of 32 columns a wavefront, with half the loads, took 29 to 32.
+// Here 16 columns see a tile of 128 tokens, 460 vector instructions: eight trees of 16
+// nodes, 64 heads on 8, 4096 tokens in 26 us.  No unit is full (vector 0.4, matrix 0.2 of
+// the launch): it is the latency of a tile's chain with 5 wavefronts a compute unit, which
+// wait for issue in a quarter of their cycles; fewer instructions shorten the chain (by 80
+// of 540: 28.8 -> 27.3).  A form of 32 columns a wavefront, with half the loads, took 29
+// to 32.
 template <int D, bool ONE, bool STREAM, bool PAIR, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int ND = D / 16;

@@ -906,10 +906,10 @@ struct Walk {
 //
 // Of few chunks it goes to the walk's end, with passes of its own in place of
 // pass_kernel's launches (5 us each, an idle one 1 to 2).  us of a call with launches /
-// so, sequences x nodes (most children), chunks:
-//   8 x 16 (4), 8: 40.9 / 25.4   32 x 24 (4), 8: 57.6 / 38.7   32 x 6 (1), 8: 30.5 / 21.4
-//   8 x 16 (4), 16: 35.5 / 28.1  32 x 24 (4), 16: 70.4 / 61.5  32 x 6 (1), 16: 33.1 / 27.1
-//   8 x 16 (4), 32: 46.4 / 51.0  32 x 24 (4), 32: 82.5 / 94.9  32 x 6 (1), 32: 38.6 / 38.5
+// so, sequences x nodes (most children), chunks, means of 6 inputs:
+//   8 x 16 (4), 8: 41.4 / 27.0   32 x 24 (4), 8: 56.4 / 40.2   32 x 6 (1), 8: 30.4 / 22.5
+//   8 x 16 (4), 16: 40.2 / 33.7  32 x 24 (4), 16: 71.9 / 66.5  32 x 6 (1), 16: 32.3 / 27.5
+//   8 x 16 (4), 32: 44.3 / 49.3  32 x 24 (4), 32: 78.2 / 95.9  32 x 6 (1), 32: 38.6 / 40.0
 constexpr uint32_t kWalkThreads = 2 * kMaxNodes, kFewChunks = 16;
 static_assert(kFewChunks <= 64);
 
@@ -1002,11 +1002,13 @@ __global__ __launch_bounds__(kWalkThreads) void walk_kernel(VerifyArgs a) {
 // its part of the sums of max(p - t q, 0) that it waits for then.  END: one block a
 // sequence, to the walk's end, by passes of its own where it has to.
 //
-// Passes by all compute units take 5.3 us for 8 sequences of 100003 logits, 8 for 32 of
-// 131072; by one block about 13.  Four of them in launches of their own: 8 trees of up
-// to 32 nodes 57.9 us in the mean of 8 inputs (three 60.4, five 59.7, eight 65.9); an
-// idle one is 1 to 2 us.  A counter and the last block to arrive in place of the next
-// launch: its fences took longer (36 us for 1024 blocks).
+// Passes by all compute units take 6 us for 8 sequences of 100003 logits, 9 for 32 of
+// 131072, of which both sums in place of one are up to 1; by one block about 13.  All
+// latency: vector units 9% busy.  Launches of their own for 3 / 4 / 5 / 8 of them, means of
+// 8 inputs: 8 trees of up to 32 nodes 53.7 / 55.6 / 57.7 / 64.8 us, with up to 8 children
+// 73.9 / 70.9 / 72.7 / 78.6, 32 of 24 nodes 99.1 / 94.5 / 93.9 / 99.5; an idle one is 1 to
+// 2.  A counter and the last block to arrive in place of the next launch took 36 us for
+// 1024 blocks, with fences by every thread; calls of few blocks were not tried.
 template <typename TT, typename TD, bool END>
 __global__ __launch_bounds__(END ? kWalkThreads : 256) void pass_kernel(VerifyArgs a, uint32_t n) {
   __shared__ Tree tree;
